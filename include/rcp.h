@@ -417,6 +417,95 @@ int rcp_gemv_w2a4_static_status(int32_t* status_host, void* stream);
  */
 int rcp_selftest_wait_timeout(void* workspace, int polls, void* stream);
 
+/*
+ * Paged cache of keys and values in 8 bits, and what a decoder layer does with it between its projections. (The paper's setting
+ * quantizes the cache as well, W2A4KV4, and prints no kernel for it; format and interface are this library's.)
+ *
+ *   k_cache, v_cache   e4m3 [pages][kv_heads][page][dim]; page: 32, 64 or 128 tokens, dim: 64 or 128.
+ *   k_scale, v_scale   fp32 [pages][kv_heads]: a value is its code times the scale of its block (a page of one head).
+ *                      Scales are powers of two between 2^-40 and 2^9, written by rcp_kv_append.
+ *   starts             int32 [seqs + 1], ascending: rows starts[b] .. starts[b+1]-1 of q, k and v are the new tokens of
+ *                      sequence b, in order. Rows in front of starts[0] and behind starts[seqs] belong to no sequence.
+ *   lengths            int32 [seqs]: tokens of the sequence, the new ones included. The last new token has position
+ *                      lengths[b] - 1. A length of zero is allowed, and no new tokens are.
+ *   table              int32 [seqs][width]: page of positions i * page .. i * page + page - 1. An entry outside
+ *                      0 .. pages - 1 is no page: tokens are not stored there and no keys are found there.
+ *   max_new            the most new tokens a sequence has (0: not known). Sets launches up, nothing more; of a sequence that has
+ *                      more, the rest is neither stored nor answered (rows left as they were).
+ * starts, lengths and table are read on the device, so a captured call serves every later step whose sizes are the same.
+ * A token without a position (lengths[b] below the number of its new tokens) or with one past width * page is not
+ * stored; its row of a result is zero.
+ * Limits (RCP_ERR_LIMIT): seqs, tokens, width * page as below.
+ */
+#define RCP_KV_MAX_SEQS 4096
+#define RCP_KV_MAX_TOKENS (1 << 20)
+#define RCP_KV_MAX_LENGTH (1 << 24)
+#define RCP_KV_MAX_HEADS 1024
+
+/*
+ * Appends the new tokens' keys and values to the cache, keys rotated by position; rotates queries on the way.
+ *   k, v       fp16 [tokens][kv_heads][dim], rows k_stride and v_stride elements apart (a multiple of 8, at least a row: parts of
+ *              a fused projection need no copy). 16-byte aligned.
+ *   rope       fp32 [rope_positions][rot/2][2]: cosine and sine of the angle of pair i at a position; NULL: no rotation.
+ *              rope_positions >= width * page. Pair i is elements i and rot/2 + i of a head, or 2i and 2i + 1 with
+ *              `interleaved`; rot a multiple of 16, at most dim (elements from rot on are not rotated).
+ *              (a, b) becomes (a c - b s, b c + a s), fp32, every product and sum rounded once. 16-byte aligned; a
+ *              constant like a layer's weights.
+ *   q, q_out   NULL, or fp16 [tokens][heads][dim]: q_out receives the rotated queries, rounded to fp16 (rows
+ *              without gaps; may be q itself if q has none). Needs rope. Rows of no sequence are left as they were.
+ * A block whose first slot is among the new tokens gets the smallest scale 2^e with max |x| <= 448 2^e over its new tokens;
+ * one that holds older tokens keeps its scale unless it has to grow, and then its older codes are rounded to the new
+ * scale. Codes: round to nearest even. Slots behind the last token are left as they were. A NaN is stored as zero,
+ * magnitudes above 2^17 as 2^17. Pages that get new tokens belong to one sequence each (two that share one race on its
+ * contents; sequences may share pages that none of them appends to).
+ * Asynchronous on `stream`; allocates nothing, needs no workspace.
+ */
+int rcp_kv_append(const void* q_f16, int64_t q_stride, const void* k_f16, int64_t k_stride, const void* v_f16, int64_t v_stride,
+                  int tokens, int heads, int kv_heads, int dim, const float* rope, int rope_positions, int rot, int interleaved,
+                  const int32_t* starts, const int32_t* lengths, const int32_t* table, int seqs, int width, int max_new,
+                  void* k_cache, void* v_cache, float* k_scale, float* v_scale, int pages, int page, void* q_out_f16,
+                  void* stream);
+
+/*
+ * Softmax attention over the cache: token at position i of a sequence attends to positions 0 .. i, its own included (append first).
+ *   out[t][h] = sum_j p_j v_j / sum_j p_j,  p_j = exp(sm_scale * (q[t][h] . k_j)),  kv head h / (heads / kv_heads)
+ *   q          fp16 [tokens][heads][dim], rows q_stride elements apart as for rcp_kv_append, rotated already.
+ *   sm_scale   finite, >= 0 (as a rule 1/sqrt(dim)).
+ *   out        fp16 [tokens][heads][dim], without gaps, 16-byte aligned. A row without keys (an empty sequence, no pages) is
+ *              zero; rows of no sequence are left as they were.
+ *   workspace  rcp_kv_attention_workspace_bytes() bytes, 16-byte aligned, zero-filled once; every call leaves it ready
+ *              for the next. Calls that may overlap on the GPU need one each.
+ * Nothing behind a sequence's length is read: slots that were never written may hold anything.
+ * Scores, maxima and sums in fp32; weights are rounded to fp16 for the product with the values, sums stay in fp32.
+ * Asynchronous on `stream`; allocates nothing.
+ */
+size_t rcp_kv_attention_workspace_bytes(void);
+int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads, int kv_heads, int dim, float sm_scale,
+                     const int32_t* starts, const int32_t* lengths, const int32_t* table, int seqs, int width, int max_new,
+                     const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale, int pages, int page,
+                     void* out_f16, void* workspace, void* stream);
+
+/*
+ * Low-rank adapters of many requests at once, beside a projection that they share (rcp_linear_w2a4 and the others here, or any
+ * other): token m uses adapter i = adapter[m],
+ *   y[m][n] = fp16( base[m][n] + scaling[i] * sum_r b[i][n][r] * (sum_k a[i][r][k] * x[m][k]) )       (fp32 arithmetic)
+ *   x        fp16 [M][K], rows x_stride elements apart (a multiple of 8, at least K); 16-byte aligned. K % 64 == 0.
+ *   a, b     fp16 [adapters][rank][K] and [adapters][N][rank], 16-byte aligned; rank a multiple of 8 up to
+ *            RCP_LORA_MAX_RANK (fill a smaller adapter up with zeros).
+ *   adapter  int32 [M]; an entry outside 0 .. adapters - 1: none, y is base.
+ *   scaling  fp32 [adapters].
+ *   base     fp16 [M][N], the projection's output; NULL: zero. May be y (the adapters are added in place).
+ *   y        fp16 [M][N]. 1 <= M <= 65535, N >= 1.
+ *   workspace  rcp_lora_workspace_bytes(M, rank) bytes, 16-byte aligned, zero-filled once; every call leaves it ready for
+ *            the next. Calls that may overlap on the GPU need one each.
+ * Asynchronous on `stream`; allocates nothing.
+ */
+#define RCP_LORA_MAX_RANK 128
+size_t rcp_lora_workspace_bytes(int M, int rank);
+int rcp_lora_add(const void* x_f16, int64_t x_stride, const void* a_f16, const void* b_f16, const int32_t* adapter,
+                 const float* scaling, const void* base_f16, int M, int N, int K, int rank, int adapters, void* y_f16,
+                 void* workspace, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -9,6 +9,7 @@ import contextlib
 import ctypes as C
 import importlib.util
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -27,6 +28,7 @@ _m = None   # the native marshalling module, bound to _lib
 _MARSHAL_PATH = marshal_path()
 _MARSHALLED = ("rcp_quantize_act", "rcp_gemv_w2a4_variant", "rcp_gemv_w2a4_grouped_variant", "rcp_gemv_w2a16_checked",
                "rcp_gemv_w3a4", "rcp_linear_w2a4_checked", "rcp_linear_w2a4_host", "rcp_gemv_workspace_bytes",
+               "rcp_kv_append", "rcp_kv_attention", "rcp_kv_attention_workspace_bytes", "rcp_lora_add", "rcp_lora_workspace_bytes",
                "rcp_header_id")
 
 
@@ -89,6 +91,17 @@ def lib():
         L.rcp_gemv_w2a16_checked.argtypes = [vp, vp, vp, i, i, i, vp, vp, vp, vp, vp, vp]
         L.rcp_linear_w2a4_checked.restype = i
         L.rcp_linear_w2a4_checked.argtypes = [vp, i, i, i, C.c_float, vp, vp, i, i, vp, vp, vp, vp, vp, vp]
+        i64 = C.c_int64
+        L.rcp_kv_append.restype = i
+        L.rcp_kv_append.argtypes = [vp, i64, vp, i64, vp, i64, i, i, i, i, vp, i, i, i, vp, vp, vp, i, i, i, vp, vp, vp, vp, i, i, vp, vp]
+        L.rcp_kv_attention_workspace_bytes.restype = u64
+        L.rcp_kv_attention_workspace_bytes.argtypes = []
+        L.rcp_kv_attention.restype = i
+        L.rcp_kv_attention.argtypes = [vp, i64, i, i, i, i, C.c_float, vp, vp, vp, i, i, i, vp, vp, vp, vp, i, i, vp, vp, vp]
+        L.rcp_lora_workspace_bytes.restype = u64
+        L.rcp_lora_workspace_bytes.argtypes = [i, i]
+        L.rcp_lora_add.restype = i
+        L.rcp_lora_add.argtypes = [vp, i64, vp, vp, vp, vp, vp, i, i, i, i, i, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -376,3 +389,71 @@ def rcp_linear_w2a4_host(x_host, had_block, clip_ratio, words, lut, y_host, x_de
     if st:
         _check("rcp_linear_w2a4_host", st)
     return y_host
+
+
+class KvCache(NamedTuple):
+    """Paged keys and values in 8 bits: codes float8_e4m3fn [pages][kv_heads][page][dim], scales float32 [pages][kv_heads]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+
+def make_kv_cache(pages: int, kv_heads: int, dim: int, page: int = 64, device="cuda") -> KvCache:
+    """An empty cache of `pages` blocks of `page` tokens (32, 64 or 128), dim 64 or 128."""
+    codes = [torch.zeros((pages, kv_heads, page, dim), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2)]
+    scales = [torch.ones((pages, kv_heads), dtype=torch.float32, device=device) for _ in range(2)]
+    return KvCache(*codes, *scales)
+
+
+def make_kv_workspace(device) -> torch.Tensor:
+    """Zero-filled scratch for rcp_kv_attention, good for all sizes; one for each stream that calls it."""
+    return torch.zeros(int(lib().rcp_kv_attention_workspace_bytes()), dtype=torch.uint8, device=device)
+
+
+def make_lora_workspace(M: int, rank: int, device) -> torch.Tensor:
+    """Zero-filled scratch for rcp_lora_add."""
+    return torch.zeros(max(16, int(lib().rcp_lora_workspace_bytes(M, rank))), dtype=torch.uint8, device=device)
+
+
+def rcp_kv_append(k, v, cache, starts, lengths, block_table, rope=None, interleaved=False, q=None, q_out=None, max_new=0):
+    """k, v fp16 [tokens][kv_heads][dim] (rows any distance apart) to the cache, k rotated by position; returns q fp16
+    [tokens][heads][dim] rotated (None without q). starts int32 [seqs + 1]: the new tokens of sequence b are rows starts[b] ..
+    starts[b+1]-1; lengths int32 [seqs]: its tokens, the new ones included; block_table int32 [seqs][width]: its pages.
+    rope float32 [positions][pairs][2]: cosine and sine. max_new: the most new tokens of a sequence, if known."""
+    if q is not None and q_out is None:
+        q_out = torch.zeros(q.shape, dtype=torch.float16, device=q.device)
+    st = (_m or _native()).kv_append(k, v, *cache, starts, lengths, block_table, rope, interleaved, q, q_out, max_new)
+    if st:
+        _check("rcp_kv_append", st)
+    return q_out if q is not None else None
+
+
+def rcp_kv_attention(q, cache, starts, lengths, block_table, sm_scale=None, max_new=0, out=None, workspace=None):
+    """Attention of the new tokens q fp16 [tokens][heads][dim] (rotated; rows any distance apart) over the cache, each over the
+    positions up to its own -> out fp16 [tokens][heads][dim]. sm_scale: 1/sqrt(dim) by default. The other arguments as for
+    rcp_kv_append, which has to come first."""
+    if out is None:
+        out = torch.zeros(q.shape, dtype=torch.float16, device=q.device)
+    if workspace is None:
+        workspace = make_kv_workspace(q.device)
+    if sm_scale is None:
+        sm_scale = q.shape[-1] ** -0.5
+    st = (_m or _native()).kv_attention(q, *cache, starts, lengths, block_table, sm_scale, max_new, out, workspace)
+    if st:
+        _check("rcp_kv_attention", st)
+    return out
+
+
+def rcp_lora_add(x, a, b, adapter, scaling, base=None, y=None, workspace=None):
+    """y fp16 [M][N] = base + scaling[i] * b[i] (a[i] x), i = adapter[m] of each token (none outside 0 .. adapters - 1).
+    x fp16 [M][K] (rows any distance apart), a fp16 [adapters][rank][K], b fp16 [adapters][N][rank], adapter int32 [M],
+    scaling float32 [adapters]; base fp16 [M][N], None (zero) or y itself."""
+    if y is None:
+        y = torch.empty((x.shape[0], b.shape[1]), dtype=torch.float16, device=x.device)
+    if workspace is None:
+        workspace = make_lora_workspace(x.shape[0], a.shape[1], x.device)
+    st = (_m or _native()).lora_add(x, a, b, adapter, scaling, base, y, workspace)
+    if st:
+        _check("rcp_lora_add", st)
+    return y

@@ -13,7 +13,8 @@ LIB = os.path.join(HERE, "librcp_w2a4.so")
 LIB_CHECKED = os.path.join(HERE, "librcp_w2a4_checked.so")   # the guarded build (-DRCP_CHECKED), for tests
 DRIVER = os.path.join(HERE, "e2e_driver")                     # host program: a decode step through the C ABI
 HEADER = os.path.join(os.path.dirname(HERE), "include", "rcp.h")
-SOURCES = ["rcp_api.cu"]
+OBJECTS = os.path.join(HERE, "_build")
+SOURCES = ["rcp_api.cu", "kv_api.cu"]
 
 
 def header_id() -> int:
@@ -35,14 +36,35 @@ def _newest_source_mtime() -> float:
     return max(os.path.getmtime(p) for p in paths)
 
 
-def _compile(out: str, defines=(), verbose: bool = False) -> str:
+def _inputs(path: str, seen=None) -> set:
+    """A source file and what it includes of this repository."""
+    seen = set() if seen is None else seen
+    path = os.path.normpath(path)
+    if path not in seen and os.path.exists(path):
+        seen.add(path)
+        for name in re.findall(r'^#include "([^"]+)"', open(path).read(), flags=re.M):
+            _inputs(os.path.join(os.path.dirname(path), name), seen)
+    return seen
+
+
+def _compile(out: str, defines=(), verbose: bool = False, force: bool = False) -> str:
+    """The sources side by side to object files (kept while nothing they include changes), then one shared library."""
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "--shared", "-Xcompiler", "-fPIC", f"-DRCP_HEADER_ID={header_id()}ull", "-o", out] + [f"-D{d}" for d in defines] + \
-          [os.path.join(CSRC, s) for s in SOURCES]
-    if verbose:
-        cmd.insert(1, "-Xptxas=-v")
-    subprocess.check_call(cmd)
+    arch = ["-gencode", "arch=compute_100a,code=sm_100a"]
+    os.makedirs(OBJECTS, exist_ok=True)
+    objects, running = [], []
+    for s in SOURCES:
+        src = os.path.join(CSRC, s)
+        obj = os.path.join(OBJECTS, "-".join([s, *defines]) + ".o")
+        objects.append(obj)
+        if not force and not verbose and os.path.exists(obj) and os.path.getmtime(obj) >= max(map(os.path.getmtime, _inputs(src))):
+            continue
+        cmd = [nvcc, *arch, "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC", f"-DRCP_HEADER_ID={header_id()}ull", "-c", "-o", obj, src]
+        running.append((cmd, subprocess.Popen(cmd + (["-Xptxas=-v"] if verbose else []) + [f"-D{d}" for d in defines])))
+    for cmd, p in running:
+        if p.wait():
+            raise subprocess.CalledProcessError(p.returncode, cmd)
+    subprocess.check_call([nvcc, *arch, "--shared", "-o", out] + objects)
     return out
 
 
@@ -51,7 +73,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     build_marshal(force)
     if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest_source_mtime():
         return LIB
-    return _compile(LIB, verbose=verbose)
+    return _compile(LIB, verbose=verbose, force=force)
 
 
 def build_checked(force: bool = False) -> str:
@@ -59,7 +81,7 @@ def build_checked(force: bool = False) -> str:
     streaming kernel checked against the host's layout; a violation is reported through the status word)."""
     if not force and os.path.exists(LIB_CHECKED) and os.path.getmtime(LIB_CHECKED) >= _newest_source_mtime():
         return LIB_CHECKED
-    return _compile(LIB_CHECKED, defines=("RCP_CHECKED",))
+    return _compile(LIB_CHECKED, defines=("RCP_CHECKED",), force=force)
 
 
 def build_marshal(force: bool = False) -> str:

@@ -5,6 +5,9 @@
 // (bind), so that the same module serves whichever build of it is loaded.
 #include <Python.h>
 
+#include <algorithm>
+#include <climits>
+
 #include <ATen/core/Tensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
@@ -27,11 +30,16 @@ struct Entry {
   decltype(&rcp_linear_w2a4_checked) linear = nullptr;
   decltype(&rcp_linear_w2a4_host) linear_host = nullptr;
   decltype(&rcp_gemv_workspace_bytes) workspace_bytes = nullptr;
+  decltype(&rcp_kv_append) kv_append = nullptr;
+  decltype(&rcp_kv_attention) kv_attention = nullptr;
+  decltype(&rcp_kv_attention_workspace_bytes) kv_workspace_bytes = nullptr;
+  decltype(&rcp_lora_add) lora_add = nullptr;
+  decltype(&rcp_lora_workspace_bytes) lora_workspace_bytes = nullptr;
 } g_fn;
 
 
 const char* type_name(at::ScalarType t) {
-  return t == at::kHalf ? "float16" : t == at::kInt ? "int32" : t == at::kFloat ? "float32" : t == at::kChar ? "int8" : "uint8";
+  return t == at::kHalf ? "float16" : t == at::kInt ? "int32" : t == at::kFloat ? "float32" : t == at::kChar ? "int8" : t == at::kFloat8_e4m3fn ? "float8_e4m3fn" : "uint8";
 }
 bool on_other_device(const char* name) {
   PyErr_Format(PyExc_ValueError, "%s: not on the device of the call's first tensor", name);
@@ -166,7 +174,10 @@ PyObject* bind(PyObject*, PyObject* table) {
   if (!take("rcp_quantize_act", g_fn.quantize_act) || !take("rcp_gemv_w2a4_variant", g_fn.gemv) ||
       !take("rcp_gemv_w2a4_grouped_variant", g_fn.gemv_grouped) || !take("rcp_gemv_w2a16_checked", g_fn.gemv_w2a16) ||
       !take("rcp_gemv_w3a4", g_fn.gemv_w3a4) || !take("rcp_linear_w2a4_checked", g_fn.linear) ||
-      !take("rcp_linear_w2a4_host", g_fn.linear_host) || !take("rcp_gemv_workspace_bytes", g_fn.workspace_bytes))
+      !take("rcp_linear_w2a4_host", g_fn.linear_host) || !take("rcp_gemv_workspace_bytes", g_fn.workspace_bytes) ||
+      !take("rcp_kv_append", g_fn.kv_append) || !take("rcp_kv_attention", g_fn.kv_attention) ||
+      !take("rcp_kv_attention_workspace_bytes", g_fn.kv_workspace_bytes) || !take("rcp_lora_add", g_fn.lora_add) ||
+      !take("rcp_lora_workspace_bytes", g_fn.lora_workspace_bytes))
     return nullptr;
   decltype(&rcp_header_id) header_id = nullptr;
   if (!take("rcp_header_id", header_id)) return nullptr;
@@ -363,9 +374,154 @@ PyObject* linear_w2a4_host(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// fp16 rows of `dims` - 1 packed dimensions, the rows any distance apart (parts of a fused projection): a TypeError otherwise
+const at::Tensor* rows(PyObject* o, const char* name, int dims, const at::Tensor* like, int64_t* stride) {
+  if (THPVariable_Check(o)) {
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (t.is_cuda() && t.scalar_type() == at::kHalf && t.dim() == dims) {
+      bool packed = t.size(dims - 1) == 1 || t.stride(dims - 1) == 1;
+      if (dims == 3) packed = packed && (t.size(1) == 1 || t.stride(1) == t.size(2));
+      if (packed) {
+        if (like && t.device() != like->device()) { on_other_device(name); return nullptr; }
+        *stride = t.size(0) == 1 ? (dims == 3 ? t.size(1) * t.size(2) : t.size(1)) : t.stride(0);
+        return &t;
+      }
+    }
+  }
+  PyErr_Format(PyExc_TypeError, "%s: expected a CUDA tensor of dtype torch.float16 with %d dimensions, all but the first without gaps", name, dims);
+  return nullptr;
+}
+// The paged cache and the sequences, as both calls on it take them: a[0..3] k, v, k_scale, v_scale; a[4..6] starts, lengths, table
+struct Cache {
+  const at::Tensor *k, *v, *ks, *vs, *starts, *lengths, *table;
+  int pages, kv_heads, page, dim, seqs, width;
+};
+bool cache_of(PyObject* const* a, const at::Tensor* like, Cache* c) {
+  if (!(c->k = dev(a[0], at::kFloat8_e4m3fn, "cache.k", like)) || !(c->v = dev(a[1], at::kFloat8_e4m3fn, "cache.v", like)) ||
+      !(c->ks = dev(a[2], at::kFloat, "cache.k_scale", like)) || !(c->vs = dev(a[3], at::kFloat, "cache.v_scale", like)) ||
+      !(c->starts = dev(a[4], at::kInt, "starts", like)) || !(c->lengths = dev(a[5], at::kInt, "lengths", like)) ||
+      !(c->table = dev(a[6], at::kInt, "block_table", like)))
+    return false;
+  const at::Tensor &k = *c->k, &t = *c->table;
+  if (k.dim() != 4 || k.sizes() != c->v->sizes() || !has_shape(*c->ks, {k.size(0), k.size(1)}) || c->ks->sizes() != c->vs->sizes())
+    return bad_shapes("the cache's codes [pages][kv_heads][page][dim] and scales [pages][kv_heads]");
+  if (t.dim() != 2 || !has_shape(*c->lengths, {t.size(0)}) || !has_shape(*c->starts, {t.size(0) + 1}))
+    return bad_shapes("starts [seqs + 1], lengths [seqs] and block_table [seqs][width]");
+  for (int64_t n : {k.size(0), k.size(1), k.size(2), k.size(3), t.size(0), t.size(1)})
+    if (n > INT_MAX) return bad_shapes("the cache and its table: a size beyond 31 bits");
+  c->pages = (int)k.size(0); c->kv_heads = (int)k.size(1); c->page = (int)k.size(2); c->dim = (int)k.size(3);
+  c->seqs = (int)t.size(0); c->width = (int)t.size(1);
+  return true;
+}
+const int32_t* ints(const at::Tensor* t) { return static_cast<const int32_t*>(t->data_ptr()); }
+
+// (k, v, cache.k, cache.v, cache.k_scale, cache.v_scale, starts, lengths, block_table, rope, interleaved, q, q_out, max_new)
+PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    Cache c;
+    int64_t ks, vs, qs = 0;
+    int interleaved, max_new;
+    void* q_out = nullptr;
+    if (!count(n, 14)) return nullptr;
+    const at::Tensor* k = rows(a[0], "k", 3, nullptr, &ks);
+    if (!k) return nullptr;
+    const at::Tensor* v = rows(a[1], "v", 3, k, &vs);
+    if (!v || !cache_of(a + 2, k, &c) || !integer(a[10], &interleaved) || !integer(a[13], &max_new)) return nullptr;
+    const int64_t T = k->size(0);
+    if (T > INT_MAX || !has_shape(*k, {T, c.kv_heads, c.dim}) || v->sizes() != k->sizes()) { bad_shapes("k, v and the cache"); return nullptr; }
+    const at::Tensor *rope = nullptr, *q = nullptr;
+    if (a[9] != Py_None) {
+      if (!(rope = dev(a[9], at::kFloat, "rope", k))) return nullptr;
+      if (rope->dim() != 3 || rope->size(2) != 2 || rope->size(0) > INT_MAX || rope->size(1) > c.dim) {
+        bad_shapes("rope and [positions][pairs][2]");
+        return nullptr;
+      }
+    }
+    int heads = c.kv_heads;
+    if (a[11] != Py_None) {
+      if (!(q = rows(a[11], "q", 3, k, &qs))) return nullptr;
+      if (q->size(0) != T || q->size(2) != c.dim || q->size(1) > INT_MAX) { bad_shapes("q, k and v"); return nullptr; }
+      heads = (int)q->size(1);
+      if (!buffer(a[12], "q_out", at::kHalf, *k, q->numel(), &q_out)) return nullptr;
+    }
+    const void *kp = k->data_ptr(), *vp = v->data_ptr(), *qp = q ? q->data_ptr() : nullptr;
+    const float* rp = rope ? static_cast<const float*>(rope->data_ptr()) : nullptr;
+    void *kc = c.k->data_ptr(), *vc = c.v->data_ptr();
+    float *ksc = static_cast<float*>(c.ks->data_ptr()), *vsc = static_cast<float*>(c.vs->data_ptr());
+    const int32_t *st = ints(c.starts), *ln = ints(c.lengths), *tb = ints(c.table);
+    const int positions = rope ? (int)rope->size(0) : 0, rot = rope ? 2 * (int)rope->size(1) : 0;
+    return on_device(*k, [&](void* stream) {
+      return g_fn.kv_append(qp, qs, kp, ks, vp, vs, (int)T, heads, c.kv_heads, c.dim, rp, positions, rot, interleaved, st, ln, tb, c.seqs, c.width,
+                            max_new, kc, vc, ksc, vsc, c.pages, c.page, q_out, stream);
+    });
+  });
+}
+
+// (q, cache.k, cache.v, cache.k_scale, cache.v_scale, starts, lengths, block_table, sm_scale, max_new, out, workspace)
+PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    Cache c;
+    int64_t qs;
+    int max_new;
+    float sm_scale;
+    void *out, *ws;
+    if (!count(n, 12)) return nullptr;
+    const at::Tensor* q = rows(a[0], "q", 3, nullptr, &qs);
+    if (!q || !cache_of(a + 1, q, &c) || !real(a[8], &sm_scale) || !integer(a[9], &max_new)) return nullptr;
+    const int64_t T = q->size(0), heads = q->size(1);
+    if (T > INT_MAX || heads > INT_MAX || q->size(2) != c.dim) { bad_shapes("q and the cache"); return nullptr; }
+    if (!buffer(a[10], "out", at::kHalf, *q, q->numel(), &out) || !buffer(a[11], "workspace", kAny, *q, (int64_t)g_fn.kv_workspace_bytes(), &ws))
+      return nullptr;
+    const void *qp = q->data_ptr(), *kc = c.k->data_ptr(), *vc = c.v->data_ptr();
+    const float *ksc = static_cast<const float*>(c.ks->data_ptr()), *vsc = static_cast<const float*>(c.vs->data_ptr());
+    const int32_t *st = ints(c.starts), *ln = ints(c.lengths), *tb = ints(c.table);
+    return on_device(*q, [&](void* stream) {
+      return g_fn.kv_attention(qp, qs, (int)T, (int)heads, c.kv_heads, c.dim, sm_scale, st, ln, tb, c.seqs, c.width, max_new, kc, vc, ksc, vsc, c.pages,
+                               c.page, out, ws, stream);
+    });
+  });
+}
+
+// (x, a, b, adapter, scaling, base, y, workspace)
+PyObject* lora_add(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    int64_t xs;
+    void *base, *y, *ws;
+    if (!count(n, 8)) return nullptr;
+    const at::Tensor* x = rows(a[0], "x", 2, nullptr, &xs);
+    if (!x) return nullptr;
+    const at::Tensor* down = dev(a[1], at::kHalf, "a", x);
+    if (!down) return nullptr;
+    const at::Tensor* up = dev(a[2], at::kHalf, "b", x);
+    if (!up) return nullptr;
+    const at::Tensor* adapter = dev(a[3], at::kInt, "adapter", x);
+    if (!adapter) return nullptr;
+    const at::Tensor* scaling = dev(a[4], at::kFloat, "scaling", x);
+    if (!scaling) return nullptr;
+    const int64_t M = x->size(0), K = x->size(1);
+    if (down->dim() != 3 || up->dim() != 3) { bad_shapes("x, a, b, adapter and scaling"); return nullptr; }
+    const int64_t L = down->size(0), R = down->size(1), N = up->size(1);
+    if (!has_shape(*down, {L, R, K}) || !has_shape(*up, {L, N, R}) || !has_shape(*adapter, {M}) || !has_shape(*scaling, {L}) || M > INT_MAX ||
+        N > INT_MAX || K > INT_MAX || L > INT_MAX) {
+      bad_shapes("x, a, b, adapter and scaling");
+      return nullptr;
+    }
+    if (!buffer(a[5], "base", at::kHalf, *x, M * N, &base) || !buffer(a[6], "y", at::kHalf, *x, M * N, &y) ||
+        !buffer(a[7], "workspace", kAny, *x, (int64_t)g_fn.lora_workspace_bytes((int)M, (int)std::min<int64_t>(R, INT_MAX)), &ws))
+      return nullptr;
+    const void *xp = x->data_ptr(), *ap = down->data_ptr(), *bp = up->data_ptr();
+    const int32_t* ip = ints(adapter);
+    const float* sp = static_cast<const float*>(scaling->data_ptr());
+    return on_device(*x, [&](void* st) {
+      return g_fn.lora_add(xp, xs, ap, bp, ip, sp, base, (int)M, (int)N, (int)K, (int)R, (int)L, y, ws, st);
+    });
+  });
+}
+
 #define RCP_FAST(fn) {#fn, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fn)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {{"bind", bind, METH_O, nullptr}, RCP_FAST(quantize_act), RCP_FAST(gemv_w2a4), RCP_FAST(gemv_w2a16),
-                          RCP_FAST(gemv_w3a4), RCP_FAST(linear_w2a4), RCP_FAST(linear_w2a4_host), {nullptr, nullptr, 0, nullptr}};
+                          RCP_FAST(gemv_w3a4), RCP_FAST(linear_w2a4), RCP_FAST(linear_w2a4_host),
+                          RCP_FAST(kv_append), RCP_FAST(kv_attention), RCP_FAST(lora_add), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,147 @@
+// C ABI of the operators beside the linear layers: the paged 8-bit cache, the attention over it, low-rank adapters.
+#include "../../include/rcp.h"
+
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <mutex>
+
+#include "api.cuh"
+#include "kv_append.cuh"
+#include "kv_attention.cuh"
+#include "lora.cuh"
+
+using namespace rcp::api;
+
+namespace {
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+// elements between rows of `width`: rows that do not overlap and start on 16 bytes
+bool stride_ok(int64_t stride, int64_t width, int rows) {
+  return stride % 8 == 0 && stride <= (int64_t(1) << 40) && (stride >= width || (rows == 1 && stride >= 0));
+}
+
+// The arguments that rcp_kv_append and rcp_kv_attention share.
+int check_cache(int tokens, int heads, int kv_heads, int dim, const int32_t* starts, const int32_t* lengths, const int32_t* table, int seqs,
+                int width, int max_new, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale, int pages, int page,
+                rcp::KvSeqs* s) {
+  if (!starts || !lengths || !table || !k_cache || !v_cache || !k_scale || !v_scale) return RCP_ERR_NULL;
+  if (tokens < 0 || heads < 1 || kv_heads < 1 || heads % kv_heads || heads > RCP_KV_MAX_HEADS || (dim != 64 && dim != 128)) return RCP_ERR_SHAPE;
+  if (seqs < 1 || width < 1 || max_new < 0 || pages < 1 || (page != 32 && page != 64 && page != 128)) return RCP_ERR_SHAPE;
+  if (seqs > RCP_KV_MAX_SEQS || tokens > RCP_KV_MAX_TOKENS || (int64_t)width * page > RCP_KV_MAX_LENGTH) return RCP_ERR_LIMIT;
+  if (!aligned16(k_cache) || !aligned16(v_cache) || !aligned4(starts) || !aligned4(lengths) || !aligned4(table) || !aligned4(k_scale) ||
+      !aligned4(v_scale))
+    return RCP_ERR_ALIGN;
+  const int lg = page == 32 ? 5 : page == 64 ? 6 : 7;
+  *s = rcp::KvSeqs{starts, lengths, table, seqs, width, page, lg, pages, tokens, max_new == 0 ? std::max(tokens, 1) : std::min(max_new, std::max(tokens, 1))};
+  return RCP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int rcp_kv_append(const void* q_f16, int64_t q_stride, const void* k_f16, int64_t k_stride, const void* v_f16, int64_t v_stride, int tokens,
+                  int heads, int kv_heads, int dim, const float* rope, int rope_positions, int rot, int interleaved, const int32_t* starts,
+                  const int32_t* lengths, const int32_t* table, int seqs, int width, int max_new, void* k_cache, void* v_cache, float* k_scale,
+                  float* v_scale, int pages, int page, void* q_out_f16, void* stream) {
+  if (!k_f16 || !v_f16 || (q_f16 && (!q_out_f16 || !rope))) return RCP_ERR_NULL;
+  rcp::AppendParams p{};
+  const int rc = check_cache(tokens, q_f16 ? heads : kv_heads, kv_heads, dim, starts, lengths, table, seqs, width, max_new, k_cache, v_cache, k_scale,
+                             v_scale, pages, page, &p.s);
+  if (rc != RCP_OK) return rc;
+  const int64_t kv_width = (int64_t)kv_heads * dim;
+  if (!stride_ok(k_stride, kv_width, tokens) || !stride_ok(v_stride, kv_width, tokens) ||
+      (q_f16 && !stride_ok(q_stride, (int64_t)heads * dim, tokens)))
+    return RCP_ERR_SHAPE;
+  // every position that the table has room for has a row of cosines
+  if (rope && (rot < 16 || rot > dim || rot % 16 || rope_positions < width * page)) return RCP_ERR_SHAPE;
+  if (!aligned16(k_f16) || !aligned16(v_f16) || !aligned16(q_f16) || !aligned16(q_out_f16) || !aligned16(rope)) return RCP_ERR_ALIGN;
+  if (tokens == 0) return RCP_OK;
+  p.q = static_cast<const __half*>(q_f16);
+  p.k = static_cast<const __half*>(k_f16);
+  p.v = static_cast<const __half*>(v_f16);
+  p.q_stride = q_stride; p.k_stride = k_stride; p.v_stride = v_stride;
+  p.rope = reinterpret_cast<const float2*>(rope);
+  p.rot = rope ? rot : 0;
+  p.interleaved = interleaved != 0;
+  p.heads = heads; p.kv_heads = kv_heads; p.dim = dim;
+  p.k_cache = static_cast<uint8_t*>(k_cache);
+  p.v_cache = static_cast<uint8_t*>(v_cache);
+  p.k_scale = k_scale; p.v_scale = v_scale;
+  p.q_out = static_cast<__half*>(q_out_f16);
+  // candidates for blocks with new tokens: so many to each sequence, or by search over starts
+  const int64_t per = (p.s.max_new + page - 2) / page + 1, direct = per * seqs, found = tokens / page + 2 * (int64_t)seqs;
+  p.direct = direct <= found ? (int)per : 0;
+  p.candidates = (int)std::min(direct, found);
+  int64_t ctas = (int64_t)p.candidates * kv_heads * 2;
+  if (q_f16) {
+    p.query_tokens = rcp::kAppendThreads / (dim / 16);
+    p.query_splits = (heads + rcp::kQueryHeads - 1) / rcp::kQueryHeads;
+    ctas += (int64_t)((tokens + p.query_tokens - 1) / p.query_tokens) * p.query_splits;
+  }
+  if (ctas > INT_MAX) return RCP_ERR_LIMIT;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const dim3 grid((unsigned)ctas), block(rcp::kAppendThreads);
+  switch (page * dim / 16 / rcp::kAppendThreads) {
+    case 1: RCP_CUDA(launch_overlapped(rcp::kv_append_kernel<1>, grid, block, 0, st, p)); break;
+    case 2: RCP_CUDA(launch_overlapped(rcp::kv_append_kernel<2>, grid, block, 0, st, p)); break;
+    case 4: RCP_CUDA(launch_overlapped(rcp::kv_append_kernel<4>, grid, block, 0, st, p)); break;
+    default: RCP_CUDA(launch_overlapped(rcp::kv_append_kernel<8>, grid, block, 0, st, p)); break;
+  }
+  return RCP_OK;
+}
+
+size_t rcp_kv_attention_workspace_bytes(void) { return 16; }
+
+int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads, int kv_heads, int dim, float sm_scale, const int32_t* starts,
+                     const int32_t* lengths, const int32_t* table, int seqs, int width, int max_new, const void* k_cache, const void* v_cache,
+                     const float* k_scale, const float* v_scale, int pages, int page, void* out_f16, void* workspace, void* stream) {
+  if (!q_f16 || !out_f16) return RCP_ERR_NULL;
+  rcp::AttnParams p{};
+  const int rc = check_cache(tokens, heads, kv_heads, dim, starts, lengths, table, seqs, width, max_new, k_cache, v_cache, k_scale, v_scale, pages,
+                             page, &p.s);
+  if (rc != RCP_OK) return rc;
+  if (!stride_ok(q_stride, (int64_t)heads * dim, tokens) || !std::isfinite(sm_scale) || sm_scale < 0.f) return RCP_ERR_SHAPE;
+  if (!aligned16(q_f16) || !aligned16(out_f16) || !aligned16(workspace)) return RCP_ERR_ALIGN;
+  if (!workspace) return RCP_ERR_WORKSPACE;
+  if (tokens == 0) return RCP_OK;
+  p.q = static_cast<const __half*>(q_f16);
+  p.q_stride = q_stride;
+  p.heads = heads; p.kv_heads = kv_heads; p.dim = dim;
+  p.scale_log2 = sm_scale * 1.4426950408889634f;
+  p.k_cache = static_cast<const uint8_t*>(k_cache);
+  p.v_cache = static_cast<const uint8_t*>(v_cache);
+  p.k_scale = k_scale; p.v_scale = v_scale;
+  p.out = static_cast<__half*>(out_f16);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const dim3 grid(tokens, heads), block(rcp::kAttnWarps * 32);
+  if (dim == 64) RCP_CUDA(launch_overlapped(rcp::kv_attention_rows_kernel<64>, grid, block, 0, st, p));
+  else RCP_CUDA(launch_overlapped(rcp::kv_attention_rows_kernel<128>, grid, block, 0, st, p));
+  return RCP_OK;
+}
+
+size_t rcp_lora_workspace_bytes(int M, int rank) {
+  if (M < 1 || M > 65535 || rank < 8 || rank > RCP_LORA_MAX_RANK || rank % 8) return 0;
+  return (size_t)M * rank * sizeof(float);
+}
+
+int rcp_lora_add(const void* x_f16, int64_t x_stride, const void* a_f16, const void* b_f16, const int32_t* adapter, const float* scaling,
+                 const void* base_f16, int M, int N, int K, int rank, int adapters, void* y_f16, void* workspace, void* stream) {
+  if (!x_f16 || !a_f16 || !b_f16 || !adapter || !scaling || !y_f16) return RCP_ERR_NULL;
+  if (!workspace) return RCP_ERR_WORKSPACE;
+  if (M < 1 || M > 65535 || N < 1 || K < 64 || K > 65536 || K % 64 || rank < 8 || rank > RCP_LORA_MAX_RANK || rank % 8 || adapters < 1)
+    return RCP_ERR_SHAPE;
+  if (!stride_ok(x_stride, K, M)) return RCP_ERR_SHAPE;
+  if (!aligned16(x_f16) || !aligned16(a_f16) || !aligned16(b_f16) || !aligned16(workspace) || !aligned4(adapter) || !aligned4(scaling) ||
+      ((reinterpret_cast<uintptr_t>(base_f16) | reinterpret_cast<uintptr_t>(y_f16)) & 1u))
+    return RCP_ERR_ALIGN;
+  rcp::LoraParams p{static_cast<const __half*>(x_f16), x_stride, static_cast<const __half*>(a_f16), static_cast<const __half*>(b_f16), adapter,
+                    scaling, static_cast<const __half*>(base_f16), static_cast<__half*>(y_f16), static_cast<float*>(workspace), M, N, K, rank, adapters};
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  RCP_CUDA(launch_overlapped(rcp::lora_down_kernel, dim3((unsigned)std::min<int64_t>(((int64_t)M * rank + 7) / 8, 148 * 8)), dim3(256), 0, st, p));
+  RCP_CUDA(launch_overlapped(rcp::lora_up_kernel, dim3((N + 255) / 256, M), dim3(256), 0, st, p));
+  return RCP_OK;
+}
+
+}  // extern "C"

@@ -8,6 +8,7 @@
 #include <mutex>
 #include <utility>
 
+#include "api.cuh"
 #include "common.cuh"
 #include "gemv_simple.cuh"
 #include "gemv_stream.cuh"
@@ -18,41 +19,9 @@
 #include "pack.cuh"
 #include "quantize_act.cuh"
 
+using namespace rcp::api;
+
 namespace {
-
-thread_local int g_last_cuda_error = 0;
-
-int cuda_fail(cudaError_t e) {
-  g_last_cuda_error = (int)e;
-  return RCP_ERR_CUDA;
-}
-
-#define RCP_CUDA(call)                            \
-  do {                                            \
-    cudaError_t e__ = (call);                     \
-    if (e__ != cudaSuccess) return cuda_fail(e__); \
-  } while (0)
-
-// Launches with programmatic stream serialization: the kernel may start while the preceding
-// kernel on the stream is still running and must execute griddepcontrol.wait before it touches
-// anything that kernel may read or write.
-template <typename... KArgs, typename... Args>
-cudaError_t launch_overlapped(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
-                              Args&&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = block;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kern, std::forward<Args>(args)...);
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 bool k_ok(int K) { return K >= 64 && K <= rcp::kMaxK && K % 64 == 0; }
 
@@ -237,8 +206,6 @@ EncodeTiledFn encode_tiled_fn() {
   return fn;
 }
 
-constexpr int kMaxDevices = 64;
-
 // Tensor maps of boxes of 16 gpcs[i] rows x 128 bytes (those with a count of 0 repeat the first). Encoding one costs the
 // host about a microsecond, so the maps of the last few (weights, shape, boxes) combinations are remembered per thread.
 int phase_maps(const uint32_t* words, int N, int K, int nphase, const int* gpcs, const rcp::GemvMaps** out) {   // gpcs [kMaxPhases]
@@ -417,34 +384,6 @@ UmmaPlan make_umma_plan(int M, int N, int K, int sms, size_t qbuf, int kp_max = 
   a = umma_plan_for(M, N, K, sms, qbuf, kp_max, 32, true, &cost[0]);
   b = umma_plan_for(M, N, K, sms, qbuf, kp_max, 48, true, &cost[1]);
   return !b.stages || (a.stages && cost[0] <= cost[1]) ? a : b;
-}
-
-// SMs of the current device (remembered per device; 148 if the query fails)
-int sm_count() {
-  static std::mutex mu;
-  static int n[kMaxDevices] = {};
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return 148;
-  std::lock_guard<std::mutex> lock(mu);
-  if (!n[dev] && cudaDeviceGetAttribute(&n[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) n[dev] = 148;
-  return n[dev];
-}
-
-// cudaFuncAttributeMaxDynamicSharedMemorySize belongs to the (kernel, device) pair: set once per device (mu and done
-// belong to the kernel)
-template <typename Kern>
-cudaError_t set_max_smem(Kern kern, int bytes, std::mutex& mu, bool (&done)[kMaxDevices]) {
-  int dev = 0;
-  const cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
-  std::lock_guard<std::mutex> lock(mu);
-  if (!done[dev]) {
-    const cudaError_t r = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (r != cudaSuccess) return r;
-    done[dev] = true;
-  }
-  return cudaSuccess;
 }
 
 template <int MODE, int MTOK, bool GRP, int FQ, bool A16, bool SPLIT, bool SDBG, bool SB, bool LATE>
@@ -1032,7 +971,7 @@ const char* rcp_status_str(int status) {
   }
 }
 
-int rcp_last_cuda_error(void) { return g_last_cuda_error; }
+int rcp_last_cuda_error(void) { return rcp::g_last_cuda_error; }
 
 #ifndef RCP_HEADER_ID
 #define RCP_HEADER_ID 0ull
