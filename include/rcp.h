@@ -437,7 +437,7 @@ int rcp_selftest_wait_timeout(void* workspace, int polls, void* stream);
  * stored; its row of a result is zero.
  * Limits (RCP_ERR_LIMIT): seqs, tokens, width * page as below.
  */
-#define RCP_KV_MAX_SEQS 4096
+#define RCP_KV_MAX_SEQS 1024
 #define RCP_KV_MAX_TOKENS (1 << 20)
 #define RCP_KV_MAX_LENGTH (1 << 24)
 #define RCP_KV_MAX_HEADS 1024

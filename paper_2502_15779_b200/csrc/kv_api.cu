@@ -37,6 +37,18 @@ int check_cache(int tokens, int heads, int kv_heads, int dim, const int32_t* sta
   return RCP_OK;
 }
 
+template <int DIM, int NT>
+int attn_split(const rcp::AttnParams& p, cudaStream_t st) {
+  using L = rcp::AttnLayout<DIM, NT>;
+  static_assert(L::bytes <= 232448, "227 KB of shared memory");
+  static std::mutex mu;
+  static bool done[kMaxDevices] = {};
+  RCP_CUDA(set_max_smem(rcp::kv_attention_split_kernel<DIM, NT>, L::bytes, mu, done));
+  RCP_CUDA(launch_overlapped(rcp::kv_attention_split_kernel<DIM, NT>, dim3(std::min(sm_count(), rcp::kAttnMaxCtas)), dim3(rcp::kAttnWarps * 32),
+                             L::bytes, st, p));
+  return RCP_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -92,7 +104,7 @@ int rcp_kv_append(const void* q_f16, int64_t q_stride, const void* k_f16, int64_
   return RCP_OK;
 }
 
-size_t rcp_kv_attention_workspace_bytes(void) { return 16; }
+size_t rcp_kv_attention_workspace_bytes(void) { return rcp::kAttnWorkspaceBytes; }
 
 int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads, int kv_heads, int dim, float sm_scale, const int32_t* starts,
                      const int32_t* lengths, const int32_t* table, int seqs, int width, int max_new, const void* k_cache, const void* v_cache,
@@ -108,17 +120,19 @@ int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads,
   if (tokens == 0) return RCP_OK;
   p.q = static_cast<const __half*>(q_f16);
   p.q_stride = q_stride;
-  p.heads = heads; p.kv_heads = kv_heads; p.dim = dim;
+  p.heads = heads; p.kv_heads = kv_heads; p.group = heads / kv_heads;
   p.scale_log2 = sm_scale * 1.4426950408889634f;
   p.k_cache = static_cast<const uint8_t*>(k_cache);
   p.v_cache = static_cast<const uint8_t*>(v_cache);
   p.k_scale = k_scale; p.v_scale = v_scale;
   p.out = static_cast<__half*>(out_f16);
+  p.arrived = static_cast<int32_t*>(workspace);
+  p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + rcp::kAttnArrivedBytes);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const dim3 grid(tokens, heads), block(rcp::kAttnWarps * 32);
-  if (dim == 64) RCP_CUDA(launch_overlapped(rcp::kv_attention_rows_kernel<64>, grid, block, 0, st, p));
-  else RCP_CUDA(launch_overlapped(rcp::kv_attention_rows_kernel<128>, grid, block, 0, st, p));
-  return RCP_OK;
+  const int64_t rows = (int64_t)p.s.max_new * p.group;
+  const int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 3;
+  if (dim == 64) return nt == 1 ? attn_split<64, 1>(p, st) : nt == 2 ? attn_split<64, 2>(p, st) : attn_split<64, 3>(p, st);
+  return nt == 1 ? attn_split<128, 1>(p, st) : nt == 2 ? attn_split<128, 2>(p, st) : attn_split<128, 3>(p, st);
 }
 
 size_t rcp_lora_workspace_bytes(int M, int rank) {

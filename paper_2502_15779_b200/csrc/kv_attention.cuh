@@ -2,7 +2,27 @@
 //
 //   out[t][h] = sum_j p_j v_j / sum_j p_j,  p_j = exp(sm_scale (q[t][h] . k_j)),  j over the positions 0 .. position of t
 //   k_j, v_j: code times the scale of its block; a page outside the cache holds no keys; a row without keys is zero.
+//
+// kv_attention_split_kernel: few rows (new tokens x query heads of a key head) a sequence, where the cache is what has to be read. Bound by
+// HBM: every code once. Rows are columns here: S^T = K Q^T and O^T = V^T P^T, so that 16 keys fill the tensor core's 16 rows
+// and eight queries its eight columns. A tile is 32 keys; codes become fp16 in registers.
+//   Fragments. Both products may take their inner index in any order that their operands share. Keys: a thread reads 16 bytes of a row
+//   (and the queries' fragments are made in that order), values: 16 bytes of each of its four tokens, whose bytes are
+//   interleaved in pairs of tokens before they are converted. The weights come out of the first product with keys along the
+//   rows and go into the second one transposed (movmatrix).
+//   Softmax. Scores in units of log2. The reference m of a row moves only when a tile has a score more than kAttnSlack above it, which
+//   a vote finds out (no reduction as a rule); weights are 2^(s - m + kAttnLift), at most 2^14 in fp16, so that weights down to 2^-22
+//   of the largest keep all their bits. The sum of the weights is one more row of the second product, of ones: what is summed is what
+//   the values are multiplied with, so the rounding of weights to fp16 cancels where they are alike.
+//   Scales are powers of two: the keys' goes into the factor of the scores, the values' into the unit of the sums, which are rescaled
+//   when the next block has another one (exactly, or by 2^-149 at the bottom).
+//   Work. Sequences x row tiles x key heads are cut into tiles of keys, and the list of all tiles is shared out evenly over warps, whatever
+//   the lengths are. A warp loads ahead through its own ring of asynchronous copies, across the ends of sequences too. What it
+//   has of a segment (the keys of one sequence, row tile and key head) in part goes to shared memory; the CTA joins what its
+//   warps have, and of a segment that goes on in other CTAs the last one to arrive joins the parts, in their order.
 #pragma once
+#include <climits>
+
 #include "common.cuh"
 #include "kv_common.cuh"
 
@@ -11,61 +31,523 @@ namespace rcp {
 struct AttnParams {
   const __half* q;
   long long q_stride;        // elements between tokens
-  int heads, kv_heads, dim;
+  int heads, kv_heads, group;   // group: query heads of a key head
   float scale_log2;          // sm_scale * log2(e)
   KvSeqs s;
   const uint8_t *k_cache, *v_cache;
   const float *k_scale, *v_scale;
   __half* out;               // [tokens][heads][dim]
+  int32_t* arrived;          // [kAttnMaxCtas], zero between calls
+  float* parts;              // [kAttnMaxCtas][2][rows][dim + 2]
 };
 
-constexpr int kAttnWarps = 4;
+constexpr int kAttnMaxCtas = 256, kAttnMaxRows = 24;
+constexpr int kAttnWarps = 8, kAttnTile = 32;
+constexpr float kAttnSlack = 6.f, kAttnLift = 8.f, kAttnNoMax = -1e30f;
+constexpr size_t kAttnArrivedBytes = kAttnMaxCtas * sizeof(int32_t);
+constexpr size_t kAttnWorkspaceBytes = kAttnArrivedBytes + (size_t)kAttnMaxCtas * 2 * kAttnMaxRows * (128 + 2) * sizeof(float);
+
+// tiles in the ring: three, or two where the parts of 24 rows leave no room
+template <int DIM, int NT>
+struct AttnLayout {
+  static constexpr int stages = DIM == 64 ? 5 : NT == 1 ? 3 : 2;
+  static constexpr int tile_bytes = kAttnTile * DIM;              // of keys, and of values
+  static constexpr int stage_bytes = 2 * tile_bytes;
+  static constexpr int rows = 8 * NT;
+  static constexpr int part_floats = rows * (DIM + 2);            // sums [rows][dim], then references and sums of weights
+  static constexpr int ring = 0, first = kAttnWarps * stages * stage_bytes;
+  static constexpr int meta = first + kAttnWarps * part_floats * 4;   // per warp and stage: scales of keys and values, whether there are any
+  static constexpr int list = meta + kAttnWarps * stages * 16;
+  static constexpr int bytes = list + 2 * kAttnWarps * 32 + 80;
+  static_assert(part_floats * 4 <= stages * stage_bytes, "a warp's last part goes where its ring was");
+  static_assert(RCP_KV_MAX_SEQS * 8 <= kAttnWarps * stages * stage_bytes, "the list of sequences' tiles lies there at first");
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ uint32_t attn_smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ uint4 lds_v4(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds_v2(uint32_t at) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  return v;
+}
+// the four e4m3 codes of a word as fp16 pairs (bytes 0, 1 and bytes 2, 3)
+__device__ __forceinline__ void e4m3_halves(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
+}
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// A place in the list of tiles: segment `seg` of sequence b (row tile seg / kv_heads, key head seg % kv_heads), tile of its keys.
+struct AttnPlace {
+  int b, seg, tile;
+  int segs, tiles;     // of the sequence: segments, tiles each
+  KvSeq sq;
+};
+template <int ROWS>
+__device__ __forceinline__ void attn_sequence(const AttnParams& p, int b, AttnPlace& at) {
+  at.b = b;
+  at.sq = kv_seq(p.s, b);
+  at.segs = (at.sq.n * p.group + ROWS - 1) / ROWS * p.kv_heads;
+  at.tiles = max(1, (at.sq.end + kAttnTile - 1) / kAttnTile);
+}
+template <int ROWS>
+__device__ __forceinline__ void attn_next_segment(const AttnParams& p, AttnPlace& at) {
+  at.tile = 0;
+  if (++at.seg < at.segs) return;
+  at.seg = 0;
+  do attn_sequence<ROWS>(p, at.b + 1, at);
+  while (at.segs == 0);
+}
+
+// what is to be done with a part of a segment in shared memory
+struct alignas(16) AttnPiece {
+  int b, seg, tile0, tiles, of, pad;   // the keys' tiles tile0 .. tile0 + tiles - 1 of `of` (tiles 0: nothing here)
+  long long start;                     // the segment's first tile in the list of all
+};
+
+// y = sums / weights as fp16, to the row's place
 template <int DIM>
-__global__ void __launch_bounds__(kAttnWarps * 32) kv_attention_rows_kernel(const AttnParams p) {
-  constexpr int PER = DIM / 32;
-  __shared__ float s_m[kAttnWarps], s_l[kAttnWarps], s_o[kAttnWarps][DIM];
+__device__ __forceinline__ __half* attn_row(const AttnParams& p, const KvSeq& sq, int seg, int rows, int row) {
+  const int r = seg / p.kv_heads * rows + row;
+  if (r >= sq.n * p.group) return nullptr;
+  const int i = r / p.group;
+  return p.out + ((long long)(sq.t0 + i) * p.heads + (long long)(seg % p.kv_heads) * p.group + (r - i * p.group)) * DIM;
+}
+
+// DIM: of a head; NT: columns of eight rows a row tile has
+template <int DIM, int NT>
+__global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(const AttnParams p) {
+  using L = AttnLayout<DIM, NT>;
+  constexpr int ROWS = L::rows, KSTEPS = DIM / 16, MT = DIM / 16, S = L::stages;
+  extern __shared__ __align__(1024) uint8_t attn_shared[];
+  const uint32_t base = attn_smem(attn_shared);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, j = lane & 3;
+  AttnPiece* const list = reinterpret_cast<AttnPiece*>(attn_shared + L::list);
+  long long* const s_sum = reinterpret_cast<long long*>(attn_shared + L::list + 2 * kAttnWarps * sizeof(AttnPiece));   // [8]: one a warp
+  int* const s_joins = reinterpret_cast<int*>(s_sum + kAttnWarps);
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int t = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (t >= p.s.starts[p.s.seqs] || t < p.s.starts[0]) return;
-  const int b = kv_find(p.s.starts, p.s.seqs, t);
-  const KvSeq sq = kv_seq(p.s, b);
-  const int i = t - sq.t0;
-  if (i >= sq.n) return;
-  const int pos = sq.first + i, end = pos < sq.end ? pos + 1 : 0, kv = h / (p.heads / p.kv_heads);
-  float q[PER], o[PER] = {}, m = -1e30f, l = 0.f;
+
+  // tiles in front of each sequence, by a scan over the sequences
+  long long* const before = reinterpret_cast<long long*>(attn_shared);
+  constexpr int PER = RCP_KV_MAX_SEQS / (kAttnWarps * 32);
+  long long mine[PER], sum = 0;
+  const int per = (p.s.seqs + kAttnWarps * 32 - 1) / (kAttnWarps * 32);
 #pragma unroll
-  for (int e = 0; e < PER; e++) q[e] = __half2float(p.q[t * p.q_stride + h * DIM + lane * PER + e]);
-  for (int j = warp; j < end; j += kAttnWarps) {
-    const int pg = p.s.table[(long long)b * p.s.width + (j >> p.s.lg_page)];
-    if (pg < 0 || pg >= p.s.pages) continue;
-    const long long block = (long long)pg * p.kv_heads + kv;
-    const long long at = (block * p.s.page + (j & (p.s.page - 1))) * DIM + lane * PER;
-    float dot = 0.f;
-#pragma unroll
-    for (int e = 0; e < PER; e++) dot = fmaf(q[e], __half2float(__half(__nv_cvt_fp8_to_halfraw(p.k_cache[at + e], __NV_E4M3))), dot);
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, x);
-    const float s = dot * (p.k_scale[block] * p.scale_log2), mn = fmaxf(m, s), f = exp2f(m - mn), w = exp2f(s - mn);
-    l = l * f + w;
-    const float wv = w * p.v_scale[block];
-#pragma unroll
-    for (int e = 0; e < PER; e++) o[e] = fmaf(wv, __half2float(__half(__nv_cvt_fp8_to_halfraw(p.v_cache[at + e], __NV_E4M3))), o[e] * f);
-    m = mn;
-  }
-  if (lane == 0) { s_m[warp] = m; s_l[warp] = l; }
-#pragma unroll
-  for (int e = 0; e < PER; e++) s_o[warp][lane * PER + e] = o[e];
-  __syncthreads();
-  if (threadIdx.x < DIM) {
-    float top = s_m[0], sum = 0.f, acc = 0.f;
-    for (int w = 1; w < kAttnWarps; w++) top = fmaxf(top, s_m[w]);
-    for (int w = 0; w < kAttnWarps; w++) {
-      const float f = exp2f(s_m[w] - top);
-      sum += s_l[w] * f;
-      acc += s_o[w][threadIdx.x] * f;
+  for (int i = 0; i < PER; i++) {
+    mine[i] = 0;
+    if (i < per && tid * per + i < p.s.seqs) {
+      AttnPlace at;
+      attn_sequence<ROWS>(p, tid * per + i, at);
+      mine[i] = (long long)at.segs * at.tiles;
     }
-    p.out[((long long)t * p.heads + h) * DIM + threadIdx.x] = __float2half_rn(sum > 0.f ? acc / sum : 0.f);
+    sum += mine[i];
+  }
+  long long upto = sum;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long o = __shfl_up_sync(0xffffffffu, upto, d);
+    if (lane >= d) upto += o;
+  }
+  if (lane == 31) s_sum[warp] = upto;
+  __syncthreads();
+  long long total = 0, run = upto - sum;
+#pragma unroll
+  for (int w = 0; w < kAttnWarps; w++) {
+    if (w < warp) run += s_sum[w];
+    total += s_sum[w];
+  }
+#pragma unroll
+  for (int i = 0; i < PER; i++) {
+    if (i < per && tid * per + i < p.s.seqs) before[tid * per + i] = run;
+    run += mine[i];
+  }
+  __syncthreads();
+  // this CTA's tiles (as many CTAs as have one for each of their warps), and this warp's among them
+  const long long ctas = min((long long)gridDim.x, (total + kAttnWarps - 1) / kAttnWarps);
+  if ((long long)blockIdx.x >= ctas) return;
+  const long long c0 = total * blockIdx.x / ctas, c1 = total * (blockIdx.x + 1) / ctas;
+  const long long w0 = c0 + (c1 - c0) * warp / kAttnWarps;
+  const int todo = (int)min(c0 + (c1 - c0) * (warp + 1) / kAttnWarps - w0, (long long)INT_MAX);
+  AttnPlace at{};
+  if (todo > 0) {
+    int lo = 0, hi = p.s.seqs;   // the last sequence with no more than w0 tiles in front: it has some itself
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (before[mid] <= w0) lo = mid; else hi = mid;
+    }
+    attn_sequence<ROWS>(p, lo, at);
+    const long long in = w0 - before[lo];
+    at.seg = (int)(in / at.tiles);
+    at.tile = (int)(in - (long long)at.seg * at.tiles);
+  }
+  if (lane < 2) list[2 * warp + lane].tiles = 0;
+  __syncthreads();
+
+  if (todo > 0) {
+    const uint32_t ring = base + (uint32_t)(warp * S * L::stage_bytes);
+    float* const metaf = reinterpret_cast<float*>(attn_shared + L::meta) + warp * S * 4;
+    AttnPlace ld = at;
+    int loaded = 0, ld_stage = 0, pages_at = -1, pages_b = -1, my_page = -1;
+    // asks for the next tile
+    auto load = [&]() {
+      if (loaded < todo) {
+        // pages of 32 tiles at a time, one a lane
+        if (ld.b != pages_b || ld.tile < pages_at || ld.tile >= pages_at + 32) {
+          pages_b = ld.b;
+          pages_at = ld.tile;
+          const int t = ld.tile + lane;
+          my_page = t * kAttnTile < ld.sq.end ? p.s.table[(long long)ld.b * p.s.width + (t * kAttnTile >> p.s.lg_page)] : -1;
+        }
+        const int pg = __shfl_sync(0xffffffffu, my_page, ld.tile - pages_at), j0 = ld.tile * kAttnTile;
+        const bool there = pg >= 0 && pg < p.s.pages;
+        const int kv = ld.seg % p.kv_heads;
+        const long long block = there ? (long long)pg * p.kv_heads + kv : 0;
+        const long long off = (block * p.s.page + (j0 & (p.s.page - 1))) * DIM;
+        const int live = there ? min(ld.sq.end - j0, kAttnTile) : 0;   // keys of the tile that exist: the others are zeroes
+        const uint32_t dst = ring + (uint32_t)(ld_stage * L::stage_bytes);
+#pragma unroll
+        for (int i = 0; i < DIM / 16; i++) {
+          const int n = lane + 32 * i, row = n / (DIM / 16), c = n % (DIM / 16);
+          const int line = DIM == 128 ? row : row >> 1, in = DIM == 128 ? c : (row & 1) * 4 + c;
+          const int kc = DIM == 128 ? in ^ ((row & 1) << 2) : in, vc = in ^ (((row >> 1) & 3) << 1);
+          const int bytes = row < live ? 16 : 0;
+          const long long from = off + (long long)(bytes ? row * DIM + c * 16 : 0);
+          cp_async16(dst + line * 128 + kc * 16, p.k_cache + from, bytes);
+          cp_async16(dst + L::tile_bytes + line * 128 + vc * 16, p.v_cache + from, bytes);
+        }
+        float* const m = metaf + ld_stage * 4;
+        if (lane == 0) cp_async4(attn_smem(m), p.k_scale + block);
+        if (lane == 1) cp_async4(attn_smem(m + 1), p.v_scale + block);
+        if (lane == 2) m[2] = there ? 1.f : 0.f;
+        loaded++;
+        if (++ld.tile == ld.tiles && loaded < todo) attn_next_segment<ROWS>(p, ld);
+      }
+      if (++ld_stage == S) ld_stage = 0;
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < S - 1; i++) load();
+
+    uint32_t q[NT][KSTEPS][2];
+    float o[MT][NT][4], l[NT][4], m[NT][2], vs = 1.f;
+    int lim[NT][2], least = 0;
+    // queries and limits of a segment; sums at zero
+    auto begin = [&]() {
+      const int kv = at.seg % p.kv_heads, r0 = at.seg / p.kv_heads * ROWS, rows = at.sq.n * p.group;
+#pragma unroll
+      for (int n = 0; n < NT; n++) {
+        const int r = r0 + n * 8 + g, i = r / p.group;
+        const bool have = r < rows;
+        const __half* const src = p.q + (have ? (long long)(at.sq.t0 + i) * p.q_stride + (long long)(kv * p.group + r - i * p.group) * DIM : 0);
+#pragma unroll
+        for (int c = 0; c < KSTEPS / 4; c++) {
+          const uint4 *v = reinterpret_cast<const uint4*>(src + 16 * (j + 4 * c));
+          const uint4 a = have ? v[0] : make_uint4(0, 0, 0, 0), b = have ? v[1] : make_uint4(0, 0, 0, 0);
+          q[n][4 * c][0] = a.x; q[n][4 * c][1] = a.y; q[n][4 * c + 1][0] = a.z; q[n][4 * c + 1][1] = a.w;
+          q[n][4 * c + 2][0] = b.x; q[n][4 * c + 2][1] = b.y; q[n][4 * c + 3][0] = b.z; q[n][4 * c + 3][1] = b.w;
+        }
+        least = n == 0 ? INT_MAX : least;
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          const int rr = r0 + n * 8 + 2 * j + e, pos = at.sq.first + rr / p.group;
+          lim[n][e] = rr >= rows ? INT_MAX : pos >= 0 && pos < at.sq.end ? pos + 1 : 0;
+          least = min(least, lim[n][e]);
+          m[n][e] = kAttnNoMax;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          l[n][e] = 0.f;
+#pragma unroll
+          for (int u = 0; u < MT; u++) o[u][n][e] = 0.f;
+        }
+      }
+      least = (int)__reduce_min_sync(0xffffffffu, least);
+      vs = 1.f;
+    };
+    // the warp's part of the segment, tiles t0 .. t1 - 1 of it: to its rows if that is all, else to shared memory
+    auto end = [&](int t0, int t1, bool last, long long unit) {   // unit: tile t1 - 1 in the list of all
+      if (t0 == 0 && t1 == at.tiles) {
+#pragma unroll
+        for (int n = 0; n < NT; n++)
+#pragma unroll
+          for (int e = 0; e < 2; e++) {
+            __half* const to = attn_row<DIM>(p, at.sq, at.seg, ROWS, n * 8 + 2 * j + e);
+            const float f = l[n][e] > 0.f ? vs / l[n][e] : l[n][e];   // no keys: zero (and a sum that is no number stays one)
+            if (to) {
+#pragma unroll
+              for (int u = 0; u < MT; u += 4) {
+                uint32_t w[4];
+#pragma unroll
+                for (int x = 0; x < 4; x++) {
+                  const __half2 h = __floats2half2_rn(o[u + x][n][e] * f, o[u + x][n][2 + e] * f);
+                  w[x] = *reinterpret_cast<const uint32_t*>(&h);
+                }
+                *reinterpret_cast<uint4*>(to + (DIM / 8) * g + 2 * u) = make_uint4(w[0], w[1], w[2], w[3]);
+              }
+            }
+          }
+        return;
+      }
+      float* const part = last ? reinterpret_cast<float*>(attn_shared + warp * S * L::stage_bytes)
+                               : reinterpret_cast<float*>(attn_shared + L::first) + warp * L::part_floats;
+#pragma unroll
+      for (int n = 0; n < NT; n++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          const int row = n * 8 + 2 * j + e;
+#pragma unroll
+          for (int u = 0; u < MT; u++)
+            *reinterpret_cast<float2*>(part + row * DIM + (DIM / 8) * g + 2 * u) = make_float2(o[u][n][e] * vs, o[u][n][2 + e] * vs);
+          if (g == 0) {
+            part[ROWS * DIM + row] = m[n][e];
+            part[ROWS * (DIM + 1) + row] = l[n][e];
+          }
+        }
+      if (lane == 0) list[2 * warp + (last ? 1 : 0)] = AttnPiece{at.b, at.seg, t0, t1 - t0, at.tiles, 0, unit + 1 - t1};
+    };
+
+    begin();
+    int stage = 0, from = at.tile;
+    for (int done = 0; done < todo; done++) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
+      __syncwarp();
+      load();
+      const uint32_t kt = ring + (uint32_t)(stage * L::stage_bytes), vt = kt + L::tile_bytes;
+      const float ks = metaf[stage * 4], vs_new = metaf[stage * 4 + 1], there = metaf[stage * 4 + 2];
+      if (++stage == S) stage = 0;
+      float s[2][NT][4];
+#pragma unroll
+      for (int t = 0; t < 2; t++) {
+#pragma unroll
+        for (int n = 0; n < NT; n++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) s[t][n][e] = 0.f;
+#pragma unroll
+        for (int c = 0; c < KSTEPS / 4; c++) {
+          uint4 x[2];
+#pragma unroll
+          for (int hf = 0; hf < 2; hf++) {
+            const int row = t * 16 + hf * 8 + g;
+            const int line = DIM == 128 ? row : row >> 1, in = DIM == 128 ? (j + 4 * c) ^ ((row & 1) << 2) : (row & 1) * 4 + j;
+            x[hf] = lds_v4(kt + line * 128 + in * 16);
+          }
+          const uint32_t w0[4] = {x[0].x, x[0].y, x[0].z, x[0].w}, w1[4] = {x[1].x, x[1].y, x[1].z, x[1].w};
+#pragma unroll
+          for (int k = 0; k < 4; k++) {
+            uint32_t a0, a1, a2, a3;
+            e4m3_halves(w0[k], a0, a2);
+            e4m3_halves(w1[k], a1, a3);
+#pragma unroll
+            for (int n = 0; n < NT; n++) mma16816(s[t][n], a0, a1, a2, a3, q[n][4 * c + k][0], q[n][4 * c + k][1]);
+          }
+        }
+      }
+      const float c = there != 0.f ? fmaxf(ks * p.scale_log2, 1e-37f) : 1.f;   // above zero: a score of -inf stays one
+      const int j0 = at.tile * kAttnTile;
+      if (there == 0.f || j0 + kAttnTile > least) {   // keys that some row does not see
+#pragma unroll
+        for (int t = 0; t < 2; t++)
+#pragma unroll
+          for (int n = 0; n < NT; n++)
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+              if (there == 0.f || j0 + t * 16 + (e >> 1) * 8 + g >= lim[n][e & 1]) s[t][n][e] = -INFINITY;
+      }
+      bool move = vs_new != vs;
+      float top[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; n++)
+#pragma unroll
+        for (int e = 0; e < 2; e++) {
+          top[n][e] = fmaxf(fmaxf(s[0][n][e], s[0][n][2 + e]), fmaxf(s[1][n][e], s[1][n][2 + e])) * c;
+          move |= top[n][e] > m[n][e] + kAttnSlack;
+        }
+      if (__any_sync(0xffffffffu, move)) {
+        const float fv = there != 0.f ? vs / vs_new : 1.f;   // a quotient of powers of two
+        if (there != 0.f) vs = vs_new;
+#pragma unroll
+        for (int n = 0; n < NT; n++)
+#pragma unroll
+          for (int e = 0; e < 2; e++) {
+            float t = top[n][e];
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, x));
+            const float mn = fmaxf(m[n][e], t), f = exp2_fast(m[n][e] - mn);
+            m[n][e] = mn;
+            l[n][e] *= f;
+#pragma unroll
+            for (int u = 0; u < MT; u++) {
+              o[u][n][e] *= f * fv;
+              o[u][n][2 + e] *= f * fv;
+            }
+          }
+      }
+      uint32_t pt[2][NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; n++) {
+        const float m0 = m[n][0] - kAttnLift, m1 = m[n][1] - kAttnLift;
+#pragma unroll
+        for (int t = 0; t < 2; t++)
+#pragma unroll
+          for (int hf = 0; hf < 2; hf++) {
+            const __half2 h = __floats2half2_rn(exp2_fast(fmaf(s[t][n][2 * hf], c, -m0)), exp2_fast(fmaf(s[t][n][2 * hf + 1], c, -m1)));
+            pt[t][n][hf] = transpose8x8(*reinterpret_cast<const uint32_t*>(&h));
+          }
+      }
+#pragma unroll
+      for (int t = 0; t < 2; t++) {
+#pragma unroll
+        for (int n = 0; n < NT; n++) mma16816(l[n], 0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u, pt[t][n][0], pt[t][n][1]);
+        uint32_t x[4][DIM / 32];   // the thread's DIM / 8 bytes of tokens 2 j, 2 j + 1, 2 j + 8, 2 j + 9
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+          const int row = t * 16 + 2 * j + (k & 1) + (k >> 1) * 8;
+          if constexpr (DIM == 128) {
+            const uint4 v = lds_v4(vt + row * 128 + ((g ^ (((row >> 1) & 3) << 1)) << 4));
+            x[k][0] = v.x; x[k][1] = v.y; x[k][2] = v.z; x[k][3] = v.w;
+          } else {
+            const uint2 v = lds_v2(vt + (row >> 1) * 128 + ((((row & 1) * 4 + (g >> 1)) ^ (((row >> 1) & 3) << 1)) << 4) + (g & 1) * 8);
+            x[k][0] = v.x; x[k][1] = v.y;
+          }
+        }
+#pragma unroll
+        for (int w = 0; w < DIM / 32; w++) {
+          uint32_t a[2][4];
+#pragma unroll
+          for (int hf = 0; hf < 2; hf++) {
+            e4m3_halves(__byte_perm(x[2 * hf][w], x[2 * hf + 1][w], 0x5140), a[0][2 * hf], a[0][2 * hf + 1]);
+            e4m3_halves(__byte_perm(x[2 * hf][w], x[2 * hf + 1][w], 0x7362), a[1][2 * hf], a[1][2 * hf + 1]);
+          }
+#pragma unroll
+          for (int n = 0; n < NT; n++) {
+            mma16816(o[2 * w][n], a[0][0], a[0][1], a[0][2], a[0][3], pt[t][n][0], pt[t][n][1]);
+            mma16816(o[2 * w + 1][n], a[1][0], a[1][1], a[1][2], a[1][3], pt[t][n][0], pt[t][n][1]);
+          }
+        }
+      }
+      if (++at.tile == at.tiles) {
+        if (done + 1 == todo) asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncwarp();
+        end(from, at.tiles, done + 1 == todo, w0 + done);
+        if (done + 1 < todo) {
+          attn_next_segment<ROWS>(p, at);
+          begin();
+          from = 0;
+        }
+      } else if (done + 1 == todo) {
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncwarp();
+        end(from, at.tile, true, w0 + done);
+      }
+    }
+  }
+  __syncthreads();
+
+  // the warps' parts: runs of the same segment are joined
+  constexpr int SLOTS = 2 * kAttnWarps, PART = L::part_floats;
+  auto part_of = [&](int slot) {
+    return reinterpret_cast<const float*>(attn_shared + ((slot & 1) ? (slot >> 1) * S * L::stage_bytes : L::first + (slot >> 1) * PART * 4));
+  };
+  for (int s0 = 0; s0 < SLOTS;) {
+    if (list[s0].tiles == 0) { s0++; continue; }
+    const AttnPiece head = list[s0];
+    int s1 = s0, tiles = 0;
+    for (; s1 < SLOTS; s1++) {
+      const AttnPiece e = list[s1];
+      if (e.tiles == 0) continue;
+      if (e.b != head.b || e.seg != head.seg) break;
+      tiles += e.tiles;
+    }
+    const KvSeq sq = kv_seq(p.s, head.b);
+    const bool whole = tiles == head.of;
+    const int slot = head.tile0 > 0 ? 0 : 1;   // of a segment that does not begin here the first slot, of one that does not end here the second
+    float* const mine = p.parts + ((size_t)blockIdx.x * 2 + slot) * PART;
+    for (int x = tid; x < ROWS * DIM / 4; x += kAttnWarps * 32) {
+      const int row = x / (DIM / 4), d = x % (DIM / 4) * 4;
+      float top = kAttnNoMax, sum = 0.f, acc[4] = {};
+      for (int s = s0; s < s1; s++)
+        if (list[s].tiles) top = fmaxf(top, part_of(s)[ROWS * DIM + row]);
+      for (int s = s0; s < s1; s++)
+        if (list[s].tiles) {
+          const float* const from = part_of(s);
+          const float f = exp2f(from[ROWS * DIM + row] - top);
+          const float4 v = *reinterpret_cast<const float4*>(from + row * DIM + d);
+          sum += from[ROWS * (DIM + 1) + row] * f;
+          acc[0] += v.x * f; acc[1] += v.y * f; acc[2] += v.z * f; acc[3] += v.w * f;
+        }
+      if (whole) {
+        __half* const to = attn_row<DIM>(p, sq, head.seg, ROWS, row);
+        const float f = sum > 0.f ? 1.f / sum : sum;
+        if (to) {
+          const __half2 a = __floats2half2_rn(acc[0] * f, acc[1] * f), b = __floats2half2_rn(acc[2] * f, acc[3] * f);
+          *reinterpret_cast<uint2*>(to + d) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+        }
+      } else {
+        __stcg(reinterpret_cast<float4*>(mine + row * DIM + d), make_float4(acc[0], acc[1], acc[2], acc[3]));
+        if (d == 0) {
+          __stcg(mine + ROWS * DIM + row, top);
+          __stcg(mine + ROWS * (DIM + 1) + row, sum);
+        }
+      }
+    }
+    if (!whole) {
+      // the last of the CTAs that have parts of this segment to arrive here joins them
+      const int first = (int)(((head.start + 1) * ctas - 1) / total), final = (int)(((head.start + head.of) * ctas - 1) / total);
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        const int n = atomicAdd(p.arrived + first, 1);
+        if (n == final - first) p.arrived[first] = 0;
+        *s_joins = n == final - first;
+      }
+      __syncthreads();
+      if (*s_joins) {
+        __threadfence();
+        for (int x = tid; x < ROWS * DIM / 4; x += kAttnWarps * 32) {
+          const int row = x / (DIM / 4), d = x % (DIM / 4) * 4;
+          __half* const to = attn_row<DIM>(p, sq, head.seg, ROWS, row);
+          if (!to) continue;
+          float top = kAttnNoMax, sum = 0.f, acc[4] = {};
+#pragma unroll 4
+          for (int c = first; c <= final; c++) top = fmaxf(top, __ldcg(p.parts + ((size_t)c * 2 + (c == first)) * PART + ROWS * DIM + row));
+#pragma unroll 4
+          for (int c = first; c <= final; c++) {
+            const float* const from = p.parts + ((size_t)c * 2 + (c == first)) * PART;
+            const float f = exp2f(__ldcg(from + ROWS * DIM + row) - top);
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(from + row * DIM + d));
+            sum += __ldcg(from + ROWS * (DIM + 1) + row) * f;
+            acc[0] += v.x * f; acc[1] += v.y * f; acc[2] += v.z * f; acc[3] += v.w * f;
+          }
+          const float f = sum > 0.f ? 1.f / sum : sum;
+          const __half2 a = __floats2half2_rn(acc[0] * f, acc[1] * f), b = __floats2half2_rn(acc[2] * f, acc[3] * f);
+          *reinterpret_cast<uint2*>(to + d) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+        }
+      }
+    }
+    s0 = s1;
   }
 }
 

@@ -42,7 +42,7 @@ def test_calls_without_tokens_are_fine(L):
 CACHE = [(NULL, dict(starts=None)), (NULL, dict(lengths=None)), (NULL, dict(table=None)), (NULL, dict(k_cache=None)), (NULL, dict(v_scale=None)),
          (SHAPE, dict(dim=96)), (SHAPE, dict(page=16)), (SHAPE, dict(page=96)), (SHAPE, dict(page=256)), (SHAPE, dict(heads=7)), (SHAPE, dict(heads=0)),
          (SHAPE, dict(kv_heads=0)), (SHAPE, dict(heads=1026, qs=1026 * 64)), (SHAPE, dict(tokens=-1)), (SHAPE, dict(seqs=0)), (SHAPE, dict(width=0)),
-         (SHAPE, dict(pages=0)), (SHAPE, dict(max_new=-1)), (LIMIT, dict(seqs=4097)), (LIMIT, dict(tokens=(1 << 20) + 1)),
+         (SHAPE, dict(pages=0)), (SHAPE, dict(max_new=-1)), (LIMIT, dict(seqs=1025)), (LIMIT, dict(tokens=(1 << 20) + 1)),
          (LIMIT, dict(width=(1 << 24) // 64 + 1)), (ALIGN, dict(k_cache=P + 8)), (ALIGN, dict(v_cache=P + 1)), (ALIGN, dict(starts=P + 2)),
          (ALIGN, dict(lengths=P + 1)), (ALIGN, dict(table=P + 2)), (ALIGN, dict(k_scale=P + 2)), (ALIGN, dict(v_scale=P + 1)),
          (SHAPE, dict(tokens=2, qs=504)), (SHAPE, dict(qs=516)), (SHAPE, dict(qs=-512)), (ALIGN, dict(q=P + 8))]
