@@ -37,6 +37,23 @@ int check_cache(int tokens, int heads, int kv_heads, int dim, const int32_t* sta
   return RCP_OK;
 }
 
+// launch_overlapped with clusters of `size` CTAs
+template <typename... KArgs, typename... Args>
+cudaError_t launch_clustered(void (*kern)(KArgs...), dim3 grid, dim3 block, int size, cudaStream_t st, Args&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim = {(unsigned)size, 1, 1};
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kern, std::forward<Args>(args)...);
+}
+
 template <int DIM, int NT>
 int attn_split(const rcp::AttnParams& p, cudaStream_t st) {
   using L = rcp::AttnLayout<DIM, NT>;
@@ -151,10 +168,24 @@ int rcp_lora_add(const void* x_f16, int64_t x_stride, const void* a_f16, const v
       ((reinterpret_cast<uintptr_t>(base_f16) | reinterpret_cast<uintptr_t>(y_f16)) & 1u))
     return RCP_ERR_ALIGN;
   rcp::LoraParams p{static_cast<const __half*>(x_f16), x_stride, static_cast<const __half*>(a_f16), static_cast<const __half*>(b_f16), adapter,
-                    scaling, static_cast<const __half*>(base_f16), static_cast<__half*>(y_f16), static_cast<float*>(workspace), M, N, K, rank, adapters};
+                    scaling, static_cast<const __half*>(base_f16), static_cast<__half*>(y_f16), static_cast<float*>(workspace), M, N, K, rank, adapters,
+                    1, N % 8 == 0 && aligned16(base_f16) && aligned16(y_f16)};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  RCP_CUDA(launch_overlapped(rcp::lora_down_kernel, dim3((unsigned)std::min<int64_t>(((int64_t)M * rank + 7) / 8, 148 * 8)), dim3(256), 0, st, p));
-  RCP_CUDA(launch_overlapped(rcp::lora_up_kernel, dim3((N + 255) / 256, M), dim3(256), 0, st, p));
+  if (M <= rcp::kLoraFew) {
+    RCP_CUDA(launch_overlapped(rcp::lora_few_kernel, dim3(M * rcp::kLoraCluster), dim3(rcp::kLoraThreads), 0, st, p));
+    return RCP_OK;
+  }
+  // as many CTAs for the parts of K as there is room for
+  const int tiles = (M + rcp::kDownTokens - 1) / rcp::kDownTokens;
+  p.parts = 8;
+  while (p.parts > 1 && (tiles * p.parts > 2 * sm_count() || p.parts > K / 64)) p.parts /= 2;
+  RCP_CUDA(launch_clustered(rcp::lora_down_kernel, dim3(tiles * p.parts), dim3(rcp::kLoraThreads), p.parts, st, p));
+  static std::mutex mu;
+  static bool done[kMaxDevices] = {};
+  RCP_CUDA(set_max_smem(rcp::lora_up_kernel, (int)sizeof(rcp::LoraUpShared), mu, done));
+  constexpr int cols = rcp::kUpCols * rcp::kUpTiles;
+  RCP_CUDA(launch_overlapped(rcp::lora_up_kernel, dim3((N + cols - 1) / cols, (M + rcp::kUpTokens - 1) / rcp::kUpTokens), dim3(rcp::kLoraThreads),
+                             sizeof(rcp::LoraUpShared), st, p));
   return RCP_OK;
 }
 
