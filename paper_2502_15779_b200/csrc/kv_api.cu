@@ -39,10 +39,11 @@ int check_cache(int tokens, int heads, int kv_heads, int dim, const int32_t* sta
 
 // launch_overlapped with clusters of `size` CTAs
 template <typename... KArgs, typename... Args>
-cudaError_t launch_clustered(void (*kern)(KArgs...), dim3 grid, dim3 block, int size, cudaStream_t st, Args&&... args) {
+cudaError_t launch_clustered(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, int size, cudaStream_t st, Args&&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -176,16 +177,17 @@ int rcp_lora_add(const void* x_f16, int64_t x_stride, const void* a_f16, const v
     return RCP_OK;
   }
   // as many CTAs for the parts of K as there is room for
-  const int tiles = (M + rcp::kDownTokens - 1) / rcp::kDownTokens;
+  const int tiles = (M + rcp::kLoraTile - 1) / rcp::kLoraTile;
   p.parts = 8;
   while (p.parts > 1 && (tiles * p.parts > 2 * sm_count() || p.parts > K / 64)) p.parts /= 2;
-  RCP_CUDA(launch_clustered(rcp::lora_down_kernel, dim3(tiles * p.parts), dim3(rcp::kLoraThreads), p.parts, st, p));
   static std::mutex mu;
   static bool done[kMaxDevices] = {};
-  RCP_CUDA(set_max_smem(rcp::lora_up_kernel, (int)sizeof(rcp::LoraUpShared), mu, done));
+  RCP_CUDA(set_max_smem(rcp::lora_down_kernel, (int)rcp::lora_down_smem(rcp::kLoraMaxRank), mu, done));
+  RCP_CUDA(launch_clustered(rcp::lora_down_kernel, dim3(tiles * p.parts), dim3(rcp::kLoraThreads), rcp::lora_down_smem(rank), p.parts, st, p));
   constexpr int cols = rcp::kUpCols * rcp::kUpTiles;
-  RCP_CUDA(launch_overlapped(rcp::lora_up_kernel, dim3((N + cols - 1) / cols, (M + rcp::kUpTokens - 1) / rcp::kUpTokens), dim3(rcp::kLoraThreads),
-                             sizeof(rcp::LoraUpShared), st, p));
+  static constexpr decltype(&rcp::lora_up_kernel<1>) up[8] = {rcp::lora_up_kernel<1>, rcp::lora_up_kernel<2>, rcp::lora_up_kernel<3>, rcp::lora_up_kernel<4>,
+                                                              rcp::lora_up_kernel<5>, rcp::lora_up_kernel<6>, rcp::lora_up_kernel<7>, rcp::lora_up_kernel<8>};
+  RCP_CUDA(launch_overlapped(up[(rank - 1) / 16], dim3((N + cols - 1) / cols, tiles), dim3(rcp::kLoraThreads), 0, st, p));
   return RCP_OK;
 }
 

@@ -185,117 +185,176 @@ __device__ __forceinline__ void lora_mma(float (&c)[4], uint32_t a0, uint32_t a1
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// the different adapters of a tile's tokens, in the order of their first token; returns how many (adapters[t] of the tokens: -1 none)
-template <int TILE>
-__device__ __forceinline__ int tile_adapters(const LoraParams& p, int m0, int (&adapter)[TILE], int (&list)[TILE], int& count) {
+constexpr int kLoraTile = 64;   // tokens of a tile
+struct LoraTokens {
+  int adapter[kLoraTile];   // of the tile's tokens, -1: none
+  int list[kLoraTile];      // the different ones
+  int count;
+};
+// Fills s; returns how many adapters there are. By one warp in a few votes (one thread with a loop took 4 us).
+__device__ __forceinline__ int tile_adapters(const LoraParams& p, int m0, LoraTokens& s) {
   const int tid = threadIdx.x;
-  if (tid < TILE) {
-    const int i = m0 + tid < p.M ? p.adapter[m0 + tid] : -1;
-    adapter[tid] = i >= 0 && i < p.adapters ? i : -1;
-  }
-  __syncthreads();
-  if (tid == 0) {
-    int n = 0;
-    for (int t = 0; t < TILE; t++) {
-      const int i = adapter[t];
-      if (i < 0 || (t > 0 && adapter[t - 1] == i)) continue;
-      bool known = false;
-      for (int k = 0; k < n; k++) known |= list[k] == i;
-      if (!known) list[n++] = i;
+  if (tid < 32) {
+    int i[2], n = 0;
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+      const int m = m0 + 32 * h + tid;
+      i[h] = m < p.M ? p.adapter[m] : -1;
+      if (i[h] < 0 || i[h] >= p.adapters) i[h] = -1;
+      s.adapter[32 * h + tid] = i[h];
     }
-    count = n;
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+      const uint32_t alike = __match_any_sync(0xffffffffu, i[h]);   // every lane has to come here, those without an adapter too
+      bool lead = i[h] >= 0 && __ffs((int)alike) - 1 == tid;
+      for (int k = 0; k < n; k++) lead = lead && s.list[k] != i[h];   // n: those of the first half
+      const uint32_t leads = __ballot_sync(0xffffffffu, lead);
+      __syncwarp();
+      if (lead) s.list[n + __popc(leads & ((1u << tid) - 1))] = i[h];
+      __syncwarp();
+      n += __popc(leads);
+    }
+    if (tid == 0) s.count = n;
   }
   __syncthreads();
-  return count;
+  return s.count;
 }
 
-constexpr int kDownTokens = 32;
-// z of kDownTokens tokens: two groups of 16 tokens x four quarters of the rank among the warps; the CTAs of a cluster have a part of K each
+__device__ __forceinline__ void lora_copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ uint4 lora_lds(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+
+constexpr int kDownStages = 4;  // of 64 elements of K: the tile's tokens, then the adapter's rows, 128 bytes each
+inline size_t lora_down_smem(int rank) { return (size_t)kDownStages * (kLoraTile + rank) * 128; }   // >= kLoraTile * rank * 4
+
+// z of a tile: four groups of 16 tokens x two halves of the rank among the warps; the CTAs of a cluster have a part of K each, through a
+// ring of asynchronous copies (fragments straight from memory took 31 us for 2011 tokens, 4096 elements, rank 64, bound by the cache's
+// ports: every row is wanted by two or four warps). Odd rows have their 64-byte halves exchanged, which keeps the reads of the fragments free
+// of bank conflicts.
 __global__ void __launch_bounds__(kLoraThreads) lora_down_kernel(const LoraParams p) {
-  __shared__ __align__(16) float s_part[kDownTokens][kLoraMaxRank];   // this CTA's part of the sums
-  __shared__ int s_adapter[kDownTokens], s_list[kDownTokens], s_count;
+  extern __shared__ __align__(128) uint8_t lora_shared[];
+  __shared__ LoraTokens s;
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, j = lane & 3;
-  const uint32_t part = cluster_rank();
-  const int m0 = (int)blockIdx.x / p.parts * kDownTokens, R = p.rank;
+  const uint32_t part = cluster_rank(), base = (uint32_t)__cvta_generic_to_shared(lora_shared);
+  const int m0 = (int)blockIdx.x / p.parts * kLoraTile, R = p.rank;
   const int chunks = p.K / 64, c0 = chunks * (int)part / p.parts, c1 = chunks * ((int)part + 1) / p.parts;
-  const int mt = warp & 1, tiles = R / 8, n0 = tiles * (warp >> 1) / 4, nn = tiles * ((warp >> 1) + 1) / 4 - n0;   // at most four
-  const int different = tile_adapters(p, m0, s_adapter, s_list, s_count);
+  const int mt = warp & 3, tiles = R / 8, n0 = warp < 4 ? 0 : tiles / 2, nn = warp < 4 ? tiles / 2 : tiles - tiles / 2;   // at most eight
+  const int stage_bytes = (kLoraTile + R) * 128;
+  const int different = tile_adapters(p, m0, s);
+  float acc[8][4];
   for (int e = 0; e < different; e++) {
-    const int i = s_list[e];
-    const __half* xr[2];
+    const int i = s.list[e];
+    // this thread's copies: 16 bytes of every 32nd row, two of tokens, up to four of the adapter
+    const int copy_row = tid >> 3, copy_to = copy_row * 128 + (((tid & 7) ^ ((copy_row & 1) << 2)) << 4);
+    const __half* from_x[2];
 #pragma unroll
-    for (int h = 0; h < 2; h++) xr[h] = p.x + (long long)min(m0 + mt * 16 + h * 8 + g, p.M - 1) * p.x_stride + 8 * j;
-    const __half* ar = p.a + ((long long)i * R + n0 * 8 + g) * p.K + 8 * j;
-    float acc[4][4] = {};
-#pragma unroll 2
+    for (int k = 0; k < 2; k++) from_x[k] = p.x + (long long)min(m0 + copy_row + 32 * k, p.M - 1) * p.x_stride + c0 * 64 + (tid & 7) * 8;
+    const __half* from_a = p.a + ((long long)i * R + copy_row) * p.K + c0 * 64 + (tid & 7) * 8;
+    int asked = c0, stage_to = 0;
+    auto load = [&]() {
+      if (asked < c1) {
+        const uint32_t dst = base + (uint32_t)(stage_to * stage_bytes + copy_to);
+#pragma unroll
+        for (int k = 0; k < 2; k++) { lora_copy16(dst + 32 * 128 * k, from_x[k]); from_x[k] += 64; }
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+          if (copy_row + 32 * k < R) lora_copy16(dst + (kLoraTile + 32 * k) * 128, from_a + (long long)32 * k * p.K);
+        from_a += 64;
+        asked++;
+      }
+      if (++stage_to == kDownStages) stage_to = 0;
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int n = 0; n < 8; n++)
+#pragma unroll
+      for (int k = 0; k < 4; k++) acc[n][k] = 0.f;
+#pragma unroll
+    for (int c = 0; c < kDownStages - 1; c++) load();
+    int stage = 0;
     for (int c = c0; c < c1; c++) {
-      uint4 xv[2][2], av[2][4];
+      asm volatile("cp.async.wait_group %0;" ::"n"(kDownStages - 2) : "memory");
+      __syncthreads();
+      load();
+      const uint32_t xs = base + (uint32_t)(stage * stage_bytes), as = xs + kLoraTile * 128;
+      if (++stage == kDownStages) stage = 0;
 #pragma unroll
       for (int q = 0; q < 2; q++) {
+        const uint32_t at = (uint32_t)(((4 * q + j) ^ ((g & 1) << 2)) << 4);
+        const uint4 u = lora_lds(xs + (mt * 16 + g) * 128 + at), v = lora_lds(xs + (mt * 16 + 8 + g) * 128 + at);
 #pragma unroll
-        for (int h = 0; h < 2; h++) xv[q][h] = ld_input(reinterpret_cast<const uint4*>(xr[h] + c * 64 + q * 32));
-#pragma unroll
-        for (int n = 0; n < 4; n++)
-          if (n < nn) av[q][n] = __ldg(reinterpret_cast<const uint4*>(ar + (long long)n * 8 * p.K + c * 64 + q * 32));
-      }
-#pragma unroll
-      for (int q = 0; q < 2; q++)
-#pragma unroll
-        for (int n = 0; n < 4; n++)
+        for (int n = 0; n < 8; n++)
           if (n < nn) {
-            lora_mma(acc[n], xv[q][0].x, xv[q][1].x, xv[q][0].y, xv[q][1].y, av[q][n].x, av[q][n].y);
-            lora_mma(acc[n], xv[q][0].z, xv[q][1].z, xv[q][0].w, xv[q][1].w, av[q][n].z, av[q][n].w);
+            const uint4 w = lora_lds(as + ((n0 + n) * 8 + g) * 128 + at);
+            lora_mma(acc[n], u.x, v.x, u.y, v.y, w.x, w.y);
+            lora_mma(acc[n], u.z, v.z, u.w, v.w, w.z, w.w);
           }
+      }
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
+    float* const out = reinterpret_cast<float*>(lora_shared);   // [tokens][rank]: no more than the ring
 #pragma unroll
-    for (int n = 0; n < 4; n++)
+    for (int n = 0; n < 8; n++)
       if (n < nn)
 #pragma unroll
         for (int h = 0; h < 2; h++) {
           const int t = mt * 16 + h * 8 + g;
-          if (s_adapter[t] == i) *reinterpret_cast<float2*>(&s_part[t][(n0 + n) * 8 + 2 * j]) = make_float2(acc[n][2 * h], acc[n][2 * h + 1]);
+          if (s.adapter[t] == i) *reinterpret_cast<float2*>(out + t * R + (n0 + n) * 8 + 2 * j) = make_float2(acc[n][2 * h], acc[n][2 * h + 1]);
         }
-  }
-  // the parts of the cluster's CTAs, each CTA a share of the sums
-  cluster_barrier();
-  const int all = kDownTokens * R;
-  for (int v = all * (int)part / p.parts + tid; v < all * ((int)part + 1) / p.parts; v += kLoraThreads) {
-    const int t = v / R, r = v - t * R, i = s_adapter[t];
-    if (i < 0) continue;
-    float sum = 0.f;
-    for (int c = 0; c < p.parts; c++) {
-      float w;
-      const uint32_t here = (uint32_t)__cvta_generic_to_shared(&s_part[t][r]);
-      asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.f32 %0, [a];\n\t}" : "=f"(w) : "r"(here), "r"(c) : "memory");
-      sum += w;
+    // the parts of the cluster's CTAs, each CTA a share of the sums
+    cluster_barrier();
+    const int all = kLoraTile * R / 4;
+    for (int v = all * (int)part / p.parts + tid; v < all * ((int)part + 1) / p.parts; v += kLoraThreads) {
+      const int t = 4 * v / R, r = 4 * v - t * R;
+      if (s.adapter[t] != i) continue;
+      const uint32_t here = base + (uint32_t)(v * 16);
+      float4 w[8];
+#pragma unroll
+      for (int c = 0; c < 8; c++) {
+        w[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c < p.parts)
+          asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\tld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [a];\n\t}"
+                       : "=f"(w[c].x), "=f"(w[c].y), "=f"(w[c].z), "=f"(w[c].w) : "r"(here), "r"(c) : "memory");
+      }
+      float4 sum = w[0];
+#pragma unroll
+      for (int c = 1; c < 8; c++) { sum.x += w[c].x; sum.y += w[c].y; sum.z += w[c].z; sum.w += w[c].w; }
+      const float f = p.scaling[i];
+      *reinterpret_cast<float4*>(p.z + (long long)(m0 + t) * R + r) = make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f);
     }
-    p.z[(long long)(m0 + t) * R + r] = sum * p.scaling[i];
+    cluster_barrier();   // nobody overwrites its ring, or ends, while others read from it
   }
-  cluster_barrier();   // no CTA ends while others read its shared memory
 }
 
-constexpr int kUpTokens = 64, kUpCols = 128, kUpTiles = 4;   // columns of a tile, tiles of a CTA
+constexpr int kUpCols = 128, kUpTiles = 8;   // columns of a tile (32 a warp), tiles of a CTA
 struct LoraUpShared {
-  __half z[2][kUpTokens][kLoraMaxRank + 16];   // upper and lower part of z / 2^exponent
-  float stage[kLoraWarps][16][64 + 4];
-  float unit[kUpTokens];
-  int adapter[kUpTokens], list[kUpTokens], count;
+  __half z[2][kLoraTile][kLoraMaxRank + 16];   // upper and lower part of z / 2^exponent
+  float unit[kLoraTile];
+  LoraTokens t;
 };
-// y of kUpTokens tokens x kUpTiles * kUpCols columns: four groups of 16 tokens x two halves of a tile's columns among the warps
-__global__ void __launch_bounds__(kLoraThreads) lora_up_kernel(const LoraParams p) {
-  extern __shared__ __align__(16) uint8_t lora_shared[];
-  LoraUpShared& s = *reinterpret_cast<LoraUpShared*>(lora_shared);
+// y of kLoraTile tokens x kUpTiles * kUpCols columns; a warp has half of the tile's tokens and 32 columns, and asks for what it adds to first. Column c of n-tile n is column
+// 8 (c / 2) + 2 n + c % 2 of the 32, so that a thread's sums of a row are eight columns side by side and meet base and y in 16 bytes.
+// STEPS: the rank in steps of 16, rounded up
+template <int STEPS>
+__global__ void __launch_bounds__(kLoraThreads, 2) lora_up_kernel(const LoraParams p) {
+  __shared__ __align__(16) LoraUpShared s;
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, j = lane & 3, R = p.rank;
-  const int m0 = (int)blockIdx.y * kUpTokens;
-  const int different = tile_adapters(p, m0, s.adapter, s.list, s.count);
+  const int m0 = (int)blockIdx.y * kLoraTile;
+  const int different = tile_adapters(p, m0, s.t);
   // four threads a token: its largest |z|, then z / 2^exponent in two parts, zeroes behind the rank (up to a multiple of 16)
   {
     const int t = tid >> 2, q = tid & 3;
-    const bool have = s.adapter[t] >= 0;
+    const bool have = s.t.adapter[t] >= 0;
     const float* const z = p.z + (long long)(m0 + t) * R;
     float top = 0.f;
     if (have)
@@ -319,71 +378,113 @@ __global__ void __launch_bounds__(kLoraThreads) lora_up_kernel(const LoraParams 
     }
   }
   __syncthreads();
-  const int mt = warp & 3, half = warp >> 2, steps = (R + 15) / 16;
-  float(*const stage)[64 + 4] = s.stage[warp];
+  const int t0 = (warp >> 2) * 32;
+  constexpr int AHEAD = STEPS < 4 ? STEPS : 4;   // steps whose part of b is asked for at once
+  // this thread's four rows: their adapters (-2: no such row) and places
+  int adapter[2][2];
+  long long row[2][2];
+#pragma unroll
+  for (int m = 0; m < 2; m++)
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+      const int t = t0 + m * 16 + h * 8 + g;
+      adapter[m][h] = m0 + t < p.M ? s.t.adapter[t] : -2;
+      row[m][h] = (long long)(m0 + t) * p.N;
+    }
   for (int tile = 0; tile < kUpTiles; tile++) {
-    const int n0 = ((int)blockIdx.x * kUpTiles + tile) * kUpCols + half * 64;
+    const int n0 = ((int)blockIdx.x * kUpTiles + tile) * kUpCols + (warp & 3) * 32;
     if (n0 >= p.N) break;
+    const int col = n0 + 8 * j;   // this thread's eight columns
+    const int nb = n0 + 8 * (g >> 1) + (g & 1);
     // adapter by adapter, the rows that have it; last the rows without any
     for (int e = 0; e <= different; e++) {
-      const int i = e < different ? s.list[e] : -1;
-      const bool mine = __any_sync(0xffffffffu, lane < 16 && m0 + mt * 16 + lane < p.M && s.adapter[mt * 16 + lane] == i);
-      if (!mine) continue;
-      if (i >= 0) {
-        float acc[8][4] = {};
-        const __half* const b = p.b + ((long long)i * p.N + n0 + g) * R + 4 * j;
-        for (int k = 0; k < steps; k++) {
-          uint2 bv[8];
+      const int i = e < different ? s.t.list[e] : -1;
+      bool mine[2][2], any = false;
 #pragma unroll
-          for (int n = 0; n < 8; n++)
-            bv[n] = n0 + n * 8 + g < p.N && 16 * k + 4 * j < R ? __ldg(reinterpret_cast<const uint2*>(b + (long long)n * 8 * R + 16 * k)) : make_uint2(0, 0);
+      for (int m = 0; m < 2; m++)
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+          mine[m][h] = adapter[m][h] == i && col < p.N;
+          any |= mine[m][h];
+        }
+      if (!__any_sync(0xffffffffu, any)) continue;
+      uint4 base[2][2];
+#pragma unroll
+      for (int m = 0; m < 2; m++)
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+          base[m][h] = make_uint4(0, 0, 0, 0);
+          if (mine[m][h] && p.base && p.wide) base[m][h] = *reinterpret_cast<const uint4*>(p.base + row[m][h] + col);
+        }
+      if (i < 0) {   // the row as it is, the signs of its zeroes too
+#pragma unroll
+        for (int m = 0; m < 2; m++)
 #pragma unroll
           for (int h = 0; h < 2; h++) {
-            const uint2 u = *reinterpret_cast<const uint2*>(&s.z[h][mt * 16 + g][16 * k + 4 * j]);
-            const uint2 v = *reinterpret_cast<const uint2*>(&s.z[h][mt * 16 + 8 + g][16 * k + 4 * j]);
+            if (!mine[m][h]) continue;
+            if (p.wide) *reinterpret_cast<uint4*>(p.y + row[m][h] + col) = base[m][h];
+            else
+              for (int k = 0; k < min(8, p.N - col); k++) p.y[row[m][h] + col + k] = p.base ? p.base[row[m][h] + col + k] : __float2half_rn(0.f);
+          }
+        continue;
+      }
+      float acc[2][4][4];
 #pragma unroll
-            for (int n = 0; n < 8; n++) lora_mma(acc[n], u.x, v.x, u.y, v.y, bv[n].x, bv[n].y);
+      for (int m = 0; m < 2; m++)
+#pragma unroll
+        for (int n = 0; n < 4; n++)
+#pragma unroll
+          for (int k = 0; k < 4; k++) acc[m][n][k] = 0.f;
+      const __half* b[4];
+#pragma unroll
+      for (int n = 0; n < 4; n++) b[n] = p.b + ((long long)i * p.N + min(nb + 2 * n, p.N - 1)) * R + 4 * j;   // (columns behind the last are dropped)
+#pragma unroll
+      for (int k0 = 0; k0 < STEPS; k0 += AHEAD) {
+        uint2 bv[AHEAD][4];
+#pragma unroll
+        for (int k = 0; k < AHEAD; k++)
+#pragma unroll
+          for (int n = 0; n < 4; n++)
+            if (k0 + k < STEPS)
+              bv[k][n] = k0 + k < STEPS - 1 || 16 * (STEPS - 1) + 4 * j < R ? __ldg(reinterpret_cast<const uint2*>(b[n] + 16 * (k0 + k))) : make_uint2(0, 0);
+#pragma unroll
+        for (int k = 0; k < AHEAD; k++)
+          if (k0 + k < STEPS)
+#pragma unroll
+            for (int m = 0; m < 2; m++)
+#pragma unroll
+              for (int h = 0; h < 2; h++) {
+                const uint2 u = *reinterpret_cast<const uint2*>(&s.z[h][t0 + m * 16 + g][16 * (k0 + k) + 4 * j]);
+                const uint2 v = *reinterpret_cast<const uint2*>(&s.z[h][t0 + m * 16 + 8 + g][16 * (k0 + k) + 4 * j]);
+#pragma unroll
+                for (int n = 0; n < 4; n++) lora_mma(acc[m][n], u.x, v.x, u.y, v.y, bv[k][n].x, bv[k][n].y);
+              }
+      }
+#pragma unroll
+      for (int m = 0; m < 2; m++)
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+          if (!mine[m][h]) continue;
+          const float unit = s.unit[t0 + m * 16 + h * 8 + g];
+          if (p.wide) {
+            float v[8];
+            halves8(base[m][h], v);
+            uint32_t w[4];
+#pragma unroll
+            for (int n = 0; n < 4; n++) {
+              const __half2 y = __floats2half2_rn(fmaf(acc[m][n][2 * h], unit, v[2 * n]), fmaf(acc[m][n][2 * h + 1], unit, v[2 * n + 1]));
+              w[n] = *reinterpret_cast<const uint32_t*>(&y);
+            }
+            *reinterpret_cast<uint4*>(p.y + row[m][h] + col) = make_uint4(w[0], w[1], w[2], w[3]);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 8; k++)
+              if (col + k < p.N) {
+                const long long at = row[m][h] + col + k;
+                p.y[at] = __float2half_rn(fmaf(acc[m][k >> 1][2 * h + (k & 1)], unit, p.base ? __half2float(p.base[at]) : 0.f));
+              }
           }
         }
-        __syncwarp();
-        const float u0 = s.unit[mt * 16 + g], u1 = s.unit[mt * 16 + 8 + g];
-#pragma unroll
-        for (int n = 0; n < 8; n++) {
-          *reinterpret_cast<float2*>(&stage[g][n * 8 + 2 * j]) = make_float2(acc[n][0] * u0, acc[n][1] * u0);
-          *reinterpret_cast<float2*>(&stage[g + 8][n * 8 + 2 * j]) = make_float2(acc[n][2] * u1, acc[n][3] * u1);
-        }
-        __syncwarp();
-      }
-      if (p.wide) {
-#pragma unroll
-        for (int q = 0; q < 4; q++) {
-          const int row = q * 4 + (lane >> 3), c = (lane & 7) * 8, m = m0 + mt * 16 + row;
-          if (m >= p.M || s.adapter[mt * 16 + row] != i || n0 + c >= p.N) continue;
-          const long long at = (long long)m * p.N + n0 + c;
-          float v[8] = {};
-          if (p.base) halves8(*reinterpret_cast<const uint4*>(p.base + at), v);
-          if (i >= 0)
-#pragma unroll
-            for (int k = 0; k < 8; k++) v[k] += stage[row][c + k];
-          uint32_t w[4];
-#pragma unroll
-          for (int k = 0; k < 4; k++) {
-            const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
-            w[k] = *reinterpret_cast<const uint32_t*>(&h);
-          }
-          *reinterpret_cast<uint4*>(p.y + at) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-      } else {
-        for (int q = 0; q < 32; q++) {
-          const int row = q >> 1, c = (q & 1) * 32 + lane, m = m0 + mt * 16 + row;
-          if (m >= p.M || s.adapter[mt * 16 + row] != i || n0 + c >= p.N) continue;
-          const long long at = (long long)m * p.N + n0 + c;
-          float v = p.base ? __half2float(p.base[at]) : 0.f;
-          if (i >= 0) v += stage[row][c];
-          p.y[at] = __float2half_rn(v);
-        }
-      }
-      __syncwarp();
     }
   }
 }
