@@ -40,6 +40,7 @@
 #include <cuda.h>
 
 #include "common.cuh"
+#include "ptx.cuh"
 #include "quantize_act.cuh"
 #include "split_act16.cuh"
 
@@ -74,7 +75,6 @@ constexpr int kGroupBytes = 16 * kChunkWords * 4; // one group's rows in a box: 
 constexpr int kStageBytes = kTileRows * kChunkWords * 4;
 constexpr int kMaxStages = 8;
 constexpr int kExpWarps = 4;                      // SB: warps that expand the activations of the stages (one per scheduler)
-constexpr uint32_t kSpinLimit = 1u << 22;         // bounded waits: give up, flag the error and exit
 
 enum GemvMode { kModeMma = 0, kModeHybrid = 1, kModeDp4a = 2 };
 
@@ -126,36 +126,6 @@ struct GemvParams {
 };
 
 // ----------------------------------------------------------------------------- PTX wrappers
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
-}
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-// Bounded wait. Returns false after `limit` polls.
-__device__ __forceinline__ bool mbar_wait_n(uint32_t bar, uint32_t parity, uint32_t limit) {
-  for (uint32_t i = 0; i < limit; i++) {
-    if (mbar_try(bar, parity)) return true;
-    __nanosleep(64);   // leave the issue slots to the warps that have work
-  }
-  return false;
-}
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) { return mbar_wait_n(bar, parity, kSpinLimit); }
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),

@@ -84,18 +84,6 @@ struct UmmaParams {
   int red_bytes, bs_bytes;
 };
 
-__device__ __forceinline__ bool elect_one() {
-  uint32_t pred;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(pred));
-  return pred != 0;
-}
-// Bounded wait of a whole warp. The vote makes the answer uniform for the compiler too: a loop that may be left lane by lane
-// loses the uniform registers that tcgen05 instructions take their operands from.
-__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity) {
-  for (uint32_t i = 0; i < kSpinLimit; i++)
-    if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
-  return false;
-}
 __device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&r)[32]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
@@ -125,11 +113,6 @@ __device__ __forceinline__ void umma(uint32_t elected, uint32_t d, uint32_t a, u
     asm volatile("{\n\t.reg .pred p, q;\n\t.reg .b64 bd;\n\tmov.b64 bd, {%2, %3};\n\tsetp.ne.b32 p, %6, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
                  "@q tcgen05.mma.cta_group::1.kind::i8 [%0], [%1], bd, %4, p;\n\t}" ::"r"(d), "r"(a), "r"(b_lo), "r"(b_hi),
                  "r"(idesc), "r"(elected), "r"(acc) : "memory");
-}
-// arrives at the barrier when the instructions this thread has issued so far are done
-__device__ __forceinline__ void umma_commit(uint32_t elected, uint32_t bar) {
-  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
-               "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(elected) : "memory");
 }
 // the 16 instructions of an item (128 codes a step, four positions each), one of its three readings
 template <bool F8>

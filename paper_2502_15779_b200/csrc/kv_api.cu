@@ -9,6 +9,7 @@
 #include "api.cuh"
 #include "kv_append.cuh"
 #include "kv_attention.cuh"
+#include "kv_attention_umma.cuh"
 #include "lora.cuh"
 
 using namespace rcp::api;
@@ -64,6 +65,19 @@ int attn_split(const rcp::AttnParams& p, cudaStream_t st) {
   RCP_CUDA(set_max_smem(rcp::kv_attention_split_kernel<DIM, NT>, L::bytes, mu, done));
   RCP_CUDA(launch_overlapped(rcp::kv_attention_split_kernel<DIM, NT>, dim3(std::min(sm_count(), rcp::kAttnMaxCtas)), dim3(rcp::kAttnWarps * 32),
                              L::bytes, st, p));
+  return RCP_OK;
+}
+
+template <int DIM>
+int attn_prompt(const rcp::AttnParams& p, cudaStream_t st) {
+  using L = rcp::PromptLayout<DIM>;
+  static_assert(L::bytes <= 232448, "227 KB of shared memory");
+  static std::mutex mu;
+  static bool done[kMaxDevices] = {};
+  RCP_CUDA(set_max_smem(rcp::kv_attention_prompt_kernel<DIM>, L::bytes, mu, done));
+  const int64_t ctas = ((int64_t)p.s.tokens * p.group / rcp::kPromptRows + p.s.seqs) * p.kv_heads;
+  if (ctas > INT_MAX) return RCP_ERR_LIMIT;
+  RCP_CUDA(launch_overlapped(rcp::kv_attention_prompt_kernel<DIM>, dim3((unsigned)ctas), dim3(rcp::kPromptThreads), L::bytes, st, p));
   return RCP_OK;
 }
 
@@ -144,10 +158,16 @@ int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads,
   p.v_cache = static_cast<const uint8_t*>(v_cache);
   p.k_scale = k_scale; p.v_scale = v_scale;
   p.out = static_cast<__half*>(out_f16);
-  p.arrived = static_cast<int32_t*>(workspace);
-  p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + rcp::kAttnArrivedBytes);
+  p.status = static_cast<int32_t*>(workspace);
+  p.arrived = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(workspace) + rcp::kAttnArrivedAt);
+  p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + rcp::kAttnPartsAt);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const int64_t rows = (int64_t)p.s.max_new * p.group;
+  int64_t rows = (int64_t)p.s.max_new * p.group;
+  if (rows > rcp::kAttnFewRows) {
+    const int rc2 = dim == 64 ? attn_prompt<64>(p, st) : attn_prompt<128>(p, st);
+    if (rc2 != RCP_OK || seqs == 1) return rc2;
+    p.few = rows = rcp::kAttnFewRows;   // and the sequences with few rows
+  }
   const int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 3;
   if (dim == 64) return nt == 1 ? attn_split<64, 1>(p, st) : nt == 2 ? attn_split<64, 2>(p, st) : attn_split<64, 3>(p, st);
   return nt == 1 ? attn_split<128, 1>(p, st) : nt == 2 ? attn_split<128, 2>(p, st) : attn_split<128, 3>(p, st);

@@ -37,6 +37,8 @@ struct AttnParams {
   const uint8_t *k_cache, *v_cache;
   const float *k_scale, *v_scale;
   __half* out;               // [tokens][heads][dim]
+  int32_t* status;           // set when a bounded wait gives up
+  int few;                   // sequences with more rows than that are not this call's (0: all are)
   int32_t* arrived;          // [kAttnMaxCtas], zero between calls
   float* parts;              // [kAttnMaxCtas][2][rows][dim + 2]
 };
@@ -44,8 +46,8 @@ struct AttnParams {
 constexpr int kAttnMaxCtas = 256, kAttnMaxRows = 24;
 constexpr int kAttnWarps = 8, kAttnTile = 32;
 constexpr float kAttnSlack = 6.f, kAttnLift = 8.f, kAttnNoMax = -1e30f;
-constexpr size_t kAttnArrivedBytes = kAttnMaxCtas * sizeof(int32_t);
-constexpr size_t kAttnWorkspaceBytes = kAttnArrivedBytes + (size_t)kAttnMaxCtas * 2 * kAttnMaxRows * (128 + 2) * sizeof(float);
+constexpr size_t kAttnArrivedAt = 256, kAttnPartsAt = kAttnArrivedAt + kAttnMaxCtas * sizeof(int32_t);
+constexpr size_t kAttnWorkspaceBytes = kAttnPartsAt + (size_t)kAttnMaxCtas * 2 * kAttnMaxRows * (128 + 2) * sizeof(float);
 
 // tiles in the ring: three, or two where the parts of 24 rows leave no room
 template <int DIM, int NT>
@@ -109,7 +111,8 @@ template <int ROWS>
 __device__ __forceinline__ void attn_sequence(const AttnParams& p, int b, AttnPlace& at) {
   at.b = b;
   at.sq = kv_seq(p.s, b);
-  at.segs = (at.sq.n * p.group + ROWS - 1) / ROWS * p.kv_heads;
+  const int rows = at.sq.n * p.group;
+  at.segs = p.few && rows > p.few ? 0 : (rows + ROWS - 1) / ROWS * p.kv_heads;
   at.tiles = max(1, (at.sq.end + kAttnTile - 1) / kAttnTile);
 }
 template <int ROWS>

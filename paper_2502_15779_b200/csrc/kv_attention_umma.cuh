@@ -1,0 +1,444 @@
+// Attention of many rows of a sequence (prompts, long guesses) over the paged 8-bit cache on tcgen05; the operator is that of
+// kv_attention.cuh, for the sequences whose new tokens times query heads of a key head are more than kAttnFewRows.
+//
+// Bound by the tensor cores and by the exponentials beside them (one for every row and key, 16 a clock and SM).
+// Work. One CTA a key head and 256 rows of a sequence (tokens x query heads that share the key head, token by token), two row tiles of 128.
+// For each tile of 128 keys: S_t = Q_t K^T (both operands in shared memory), weights to tensor memory as fp16 in the place of the scores,
+// O_t += P_t V (weights from tensor memory). Scores and sums of both row tiles fill tensor memory: 2 (128 + dim) columns.
+// Warps. Four that turn codes into fp16, once for all 256 rows, from memory through registers into shared memory (128-byte
+// swizzle; values keep their order, keys along the rows, and are read as a transposed operand); two that issue, one a row tile, so that neither waits for the
+// other's softmax; eight for the softmax, one thread a row. While one row tile's weights are made, the tensor cores work on the other.
+// Softmax as in kv_attention.cuh: a row's reference moves only when a score is more than kAttnSlack above it, the sums in tensor memory
+// are rescaled then. The scales of the values' blocks are folded into the fp16 values relative to a power of two, the unit of the
+// sums, which stays while every block's exponent is within -11 .. 7 of it (fp16 then holds all codes exactly) and moves otherwise; converters
+// and softmax warps follow the same rule on the same scales, so nothing has to be handed over.
+#pragma once
+#include "kv_attention.cuh"
+#include "ptx.cuh"
+
+namespace rcp {
+
+constexpr int kPromptThreads = 512, kPromptRows = 256, kPromptKeys = 128;
+constexpr int kAttnFewRows = 64;   // sequences with no more rows than that go to kv_attention_split_kernel
+
+constexpr uint32_t kPromptPolls = 1u << 18;   // a wait of this kernel is a few microseconds
+
+template <int DIM>
+struct PromptLayout {
+  static constexpr int tile_bytes = kPromptKeys * DIM * 2;   // 128 rows in fp16: blocks of 64 elements, 128 bytes a row each
+  static constexpr int q = 0, k = 2 * tile_bytes, v = k + 2 * tile_bytes, bars = v + 2 * tile_bytes;
+  static constexpr int bytes = bars + 256 + 1024;            // the swizzle wants 1024-byte alignment
+};
+
+__device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
+      "%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]),
+        "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at), "r"(r[0]),
+               "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+               "r"(r[13]), "r"(r[14]), "r"(r[15])
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st32w(uint32_t at, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(at),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+      "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
+      "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+// fp32 += fp16 x fp16; A from shared memory or from tensor memory (at `a`)
+__device__ __forceinline__ void umma_ss(uint32_t elected, uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n\t.reg .pred p, q;\n\t.reg .b64 ad, bd;\n\tmov.b64 ad, {%1, %3};\n\tmov.b64 bd, {%2, %3};\n\tsetp.ne.b32 p, %6, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+               "@q tcgen05.mma.cta_group::1.kind::f16 [%0], ad, bd, %4, p;\n\t}" ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(elected), "r"(acc)
+               : "memory");
+}
+__device__ __forceinline__ void umma_ts(uint32_t elected, uint32_t d, uint32_t a, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n\t.reg .pred p, q;\n\t.reg .b64 bd;\n\tmov.b64 bd, {%2, %3};\n\tsetp.ne.b32 p, %6, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+               "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], bd, %4, p;\n\t}" ::"r"(d), "r"(a), "r"(b_lo), "r"(hi), "r"(idesc), "r"(elected), "r"(acc)
+               : "memory");
+}
+
+__device__ __forceinline__ bool prompt_wait(uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, kPromptPolls); }
+
+// Pages and scales of a sequence's keys in units of 32, one unit a lane, 32 units (eight tiles) at a time; the next 32 are asked for ahead.
+struct PromptBlocks {
+  const KvSeqs* s;
+  const int32_t* row;                 // the sequence's row of the table
+  const float *k_scale, *v_scale;
+  int kv, kv_heads, end, lane;
+  int page, next_page;                // -1: none
+  float ks, next_ks;
+  int ve, next_ve;                    // exponent of the values' scale
+  int unit;                           // exponent of the unit of the sums; INT_MIN in front of the first tile
+
+  __device__ __forceinline__ int find(int at) const {   // page of keys 32 at ..
+    if (at * 32 >= end) return -1;
+    const int pg = row[at * 32 >> s->lg_page];
+    return pg >= 0 && pg < s->pages ? pg : -1;
+  }
+  __device__ __forceinline__ void scales(int pg, float& k, int& v) const {
+    k = pg >= 0 ? k_scale[(long long)pg * kv_heads + kv] : 1.f;
+    v = pg >= 0 ? kv_stored_exponent(v_scale[(long long)pg * kv_heads + kv]) : INT_MIN;
+  }
+  __device__ __forceinline__ void start() {
+    next_page = find(lane);
+    scales(next_page, next_ks, next_ve);
+    unit = INT_MIN;
+  }
+  // to be called for every tile in turn; returns by how many powers of two the sums' unit grows with it (0 as a rule)
+  __device__ __forceinline__ int step(int tile) {
+    if ((tile & 7) == 0) {
+      page = next_page; ks = next_ks; ve = next_ve;
+      next_page = find((tile + 8) * 4 + lane);
+    }
+    if ((tile & 7) == 4) scales(next_page, next_ks, next_ve);
+    const int at = (tile & 7) * 4;
+    const int top = __reduce_max_sync(0xffffffffu, lane >= at && lane < at + 4 ? ve : INT_MIN);
+    if (top == INT_MIN) return 0;                       // no keys in this tile
+    if (unit != INT_MIN && top - unit <= 7 && top - unit >= -11) return 0;
+    const int grow = unit == INT_MIN ? 0 : top + 4 - unit;
+    unit = top + 4;
+    return grow;
+  }
+};
+
+template <int DIM>
+__global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(const AttnParams p) {
+  using L = PromptLayout<DIM>;
+  constexpr int BLOCK = kPromptKeys * 128;   // bytes of a 64-element block of 128 rows
+  extern __shared__ uint8_t prompt_raw[];
+  __shared__ uint32_t s_tmem;
+  const uint32_t raw = smem_u32(prompt_raw), base = (raw + 1023u) & ~1023u;
+  uint8_t* const gen = prompt_raw + (base - raw);
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+
+  // which sequence and rows: candidate floor(starts[b] group / 256) + b + j is tile j of sequence b; the last ones first, they have most keys
+  const int kv = (int)blockIdx.x % p.kv_heads, cand = (int)(gridDim.x / p.kv_heads) - 1 - (int)blockIdx.x / p.kv_heads;
+  int lo = 0, hi = p.s.seqs;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if ((int)((long long)p.s.starts[mid] * p.group / kPromptRows) + mid <= cand) lo = mid; else hi = mid;
+  }
+  const KvSeq sq = kv_seq(p.s, lo);
+  const int b = lo, tile_row = (cand - (int)((long long)p.s.starts[b] * p.group / kPromptRows) - b) * kPromptRows;
+  const int total_rows = sq.n * p.group, rows = min(total_rows - tile_row, kPromptRows);
+  // few rows are the other kernel's (which runs beside this one unless there is but one sequence). Behind a wait that gave up nothing
+  // more is waited for: the results are invalid already.
+  const int gave_up = __syncthreads_or(tid == 0 && *reinterpret_cast<volatile int32_t*>(p.status) != 0);
+  if (gave_up || tile_row < 0 || rows <= 0 || (p.s.seqs > 1 && total_rows <= kAttnFewRows)) {
+    asm volatile("griddepcontrol.launch_dependents;");
+    return;
+  }
+  const int last_pos = sq.first + (tile_row + rows - 1) / p.group;
+  const int keys = min(max(last_pos + 1, 0), sq.end), tiles = (keys + kPromptKeys - 1) / kPromptKeys;
+  const int halves = rows > 128 ? 2 : 1;
+
+  const uint32_t bar = base + L::bars;
+  const uint32_t k_full = bar, k_empty = bar + 16, v_full = bar + 32, v_empty = bar + 48;   // two stages each
+  const uint32_t s_full = bar + 64, p_full = bar + 80, o_done = bar + 96, drained = bar + 112;   // one for each row tile
+  if (tid == 0) {
+    for (int i = 0; i < 2; i++) {
+      mbar_init(k_full + 8 * i, 128);
+      mbar_init(k_empty + 8 * i, halves);
+      mbar_init(v_full + 8 * i, 128);
+      mbar_init(v_empty + 8 * i, halves);
+      mbar_init(s_full + 8 * i, 1);
+      mbar_init(p_full + 8 * i, 128);
+      mbar_init(o_done + 8 * i, 1);
+      mbar_init(drained + 8 * i, 1);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 15) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  // queries, 16 bytes at a time; rows that do not exist are zeroes
+  for (int x = tid; x < halves * 128 * (DIM / 8); x += kPromptThreads) {
+    const int row = x / (DIM / 8), c = x % (DIM / 8), r = tile_row + row, i = r / p.group;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (row < rows)
+      v = *reinterpret_cast<const uint4*>(p.q + (long long)(sq.t0 + i) * p.q_stride + (long long)(kv * p.group + r - i * p.group) * DIM + 8 * c);
+    *reinterpret_cast<uint4*>(gen + L::q + (row >> 7) * L::tile_bytes + (c >> 3) * BLOCK + (row & 127) * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  // the next kernel may start when every CTA has its tensor memory: one that waits for this one must not hold what this one wants
+  asm volatile("griddepcontrol.launch_dependents;");
+
+  PromptBlocks blocks;
+  blocks.s = &p.s;
+  blocks.row = p.s.table + (long long)b * p.s.width;
+  blocks.k_scale = p.k_scale; blocks.v_scale = p.v_scale;
+  blocks.kv = kv; blocks.kv_heads = p.kv_heads; blocks.end = sq.end; blocks.lane = lane;
+  constexpr uint32_t kS = 0, kO = 256;   // tensor memory: scores (and weights) of the row tiles, then their sums
+  bool ok = true;
+
+  if (warp < 8) {
+    // ---------------------------------------------------------------- softmax: a thread a row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+    const int half = warp >> 2;
+    if (half < halves) {
+      const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, at_s = kS + 128u * half + lanes, at_o = kO + (uint32_t)(DIM * half) + lanes;
+      const int r = tile_row + half * 128 + (warp & 3) * 32 + lane;
+      const bool have = r < total_rows;
+      const int i = r / p.group, pos = sq.first + i;
+      const int lim = !have ? INT_MAX : pos >= 0 && pos < sq.end ? pos + 1 : 0;   // keys the row sees
+      const int least = (int)__reduce_min_sync(0xffffffffu, lim);
+      float m = kAttnNoMax, l = 0.f;
+      blocks.start();
+      for (int t = 0; t < tiles; t++) {
+        const int grow = blocks.step(t);
+        float c[4];
+        bool some = true;
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+          const int from = (t & 7) * 4 + k;
+          c[k] = fmaxf(__shfl_sync(0xffffffffu, blocks.ks, from) * p.scale_log2, 1e-37f);   // above zero: a score of -inf stays one
+          some = some && __shfl_sync(0xffffffffu, blocks.page, from) >= 0;
+        }
+        ok = prompt_wait(s_full + 8 * half, t & 1);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        uint32_t s[4][32];
+#pragma unroll
+        for (int k = 0; k < 4; k++) tmem_ld32(at_s + 32u * k, s[k]);
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        if (!some || (t + 1) * kPromptKeys > least) {   // keys that some row of the warp does not see, or that are not there
+#pragma unroll
+          for (int k = 0; k < 4; k++) {
+            const bool there = __shfl_sync(0xffffffffu, blocks.page, (t & 7) * 4 + k) >= 0;
+            const int left = there ? lim - t * kPromptKeys - 32 * k : 0;
+#pragma unroll
+            for (int x = 0; x < 32; x++)
+              if (x >= left) s[k][x] = 0xFF800000u;
+          }
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+          float a[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int x = 0; x < 32; x++) a[x & 3] = fmaxf(a[x & 3], __uint_as_float(s[k][x]));
+          top = fmaxf(top, fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])) * c[k]);
+        }
+        if (__any_sync(0xffffffffu, top > m + kAttnSlack || grow != 0)) {
+          const float mn = fmaxf(m, top), f = exp2_fast(m - mn);
+          m = mn;
+          l *= f;
+          // (the product into O of the tile in front is done: the scores of this one were asked for behind it)
+          const float fu = f * kv_pow2(min(max(-grow, -100), 100));
+          if (t > 0) {
+#pragma unroll
+            for (int d = 0; d < DIM / 32; d++) {
+              uint32_t o[32];
+              tmem_ld32(at_o + 32u * d, o);
+              asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+              for (int x = 0; x < 32; x++) o[x] = __float_as_uint(__uint_as_float(o[x]) * fu);
+              tmem_st32w(at_o + 32u * d, o);
+            }
+          }
+        }
+        const float ref = m - kAttnLift;
+        float sum[4] = {};
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+          uint32_t w[16];
+#pragma unroll
+          for (int x = 0; x < 16; x++) {
+            const float e0 = exp2_fast(fmaf(__uint_as_float(s[k][2 * x]), c[k], -ref)), e1 = exp2_fast(fmaf(__uint_as_float(s[k][2 * x + 1]), c[k], -ref));
+            const __half2 h = __floats2half2_rn(e0, e1);
+            w[x] = *reinterpret_cast<const uint32_t*>(&h);
+            sum[(2 * x) & 3] += e0;
+            sum[(2 * x + 1) & 3] += e1;
+          }
+          tmem_st16(at_s + 16u * k, w);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        mbar_arrive(p_full + 8 * half);
+      }
+      if (ok && tiles > 0) ok = prompt_wait(o_done + 8 * half, (tiles - 1) & 1);
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      if (ok) {
+        __half* const to = p.out + ((long long)(sq.t0 + i) * p.heads + (long long)kv * p.group + (r - i * p.group)) * DIM;
+        const float f = l > 0.f ? kv_pow2(min(max(blocks.unit, -100), 100)) / l : l;
+#pragma unroll
+        for (int d = 0; d < DIM / 32; d++) {
+          uint32_t o[32];
+          if (tiles > 0) {
+            tmem_ld32(at_o + 32u * d, o);
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          }
+          if (have) {
+#pragma unroll
+            for (int x = 0; x < 4; x++) {
+              uint32_t w[4];
+#pragma unroll
+              for (int k = 0; k < 4; k++) {
+                const __half2 h = tiles > 0 && l != 0.f ? __floats2half2_rn(__uint_as_float(o[8 * x + 2 * k]) * f, __uint_as_float(o[8 * x + 2 * k + 1]) * f)
+                                                        : __floats2half2_rn(0.f, 0.f);
+                w[k] = *reinterpret_cast<const uint32_t*>(&h);
+              }
+              *reinterpret_cast<uint4*>(to + 32 * d + 8 * x) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          }
+        }
+      }
+    }
+  } else if (warp < 12) {
+    // ---------------------------------------------------------------- converters
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 112;");
+    constexpr int PIECES = DIM / 16, COPIES = PIECES;   // 16-byte pieces of codes: of a row, and of a thread (128 rows x PIECES / 128 threads)
+    const int me = tid - 256;
+    blocks.start();
+    uint4 codes[2][COPIES];   // keys, values: asked for a tile ahead
+    int pages[4];
+    auto ask = [&](int t, uint4 (&to)[COPIES], const uint8_t* cache) {
+#pragma unroll
+      for (int k = 0; k < COPIES; k++) {
+        const int n = me + 128 * k, row = n / PIECES, piece = n % PIECES, j = t * kPromptKeys + row;
+        // the row's unit of 32 keys does not depend on the thread: 128 / PIECES rows a step
+        const int pg = pages[k * (128 / PIECES) >> 5];
+        to[k] = make_uint4(0, 0, 0, 0);
+        if (pg >= 0 && j < sq.end)
+          to[k] = __ldcg(reinterpret_cast<const uint4*>(cache + (((long long)pg * p.kv_heads + kv) * p.s.page + (j & (p.s.page - 1))) * DIM + 16 * piece));
+      }
+    };
+    auto put = [&](const uint4 (&from)[COPIES], uint32_t dst, bool values, const int (&shift)[4]) {
+#pragma unroll
+      for (int k = 0; k < COPIES; k++) {
+        const int n = me + 128 * k, row = n / PIECES, piece = n % PIECES;
+        uint32_t h[8];
+        e4m3_halves(from[k].x, h[0], h[1]);
+        e4m3_halves(from[k].y, h[2], h[3]);
+        e4m3_halves(from[k].z, h[4], h[5]);
+        e4m3_halves(from[k].w, h[6], h[7]);
+        if (values) {
+          const __half2 f = __float2half2_rn(kv_pow2(min(max(shift[k * (128 / PIECES) >> 5], -30), 7)));
+#pragma unroll
+          for (int x = 0; x < 8; x++) {
+            const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&h[x]), f);
+            h[x] = *reinterpret_cast<const uint32_t*>(&y);
+          }
+        }
+        // 16 elements are two pieces of 16 bytes; the second block's threads begin with the second one, other banks than the first block's
+        const uint32_t at = dst + (uint32_t)((piece >> 2) * BLOCK + row * 128);
+        const uint32_t c = (uint32_t)((piece & 3) * 2), odd = (uint32_t)(piece >> 2) & 1u, r7 = (uint32_t)row & 7u;
+        const uint4 first = odd ? make_uint4(h[4], h[5], h[6], h[7]) : make_uint4(h[0], h[1], h[2], h[3]);
+        const uint4 second = odd ? make_uint4(h[0], h[1], h[2], h[3]) : make_uint4(h[4], h[5], h[6], h[7]);
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at + (((c + odd) ^ r7) << 4)), "r"(first.x), "r"(first.y), "r"(first.z), "r"(first.w)
+                     : "memory");
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at + (((c + 1 - odd) ^ r7) << 4)), "r"(second.x), "r"(second.y), "r"(second.z), "r"(second.w)
+                     : "memory");
+      }
+    };
+    int shift[4];
+    // pages of tile t, and how far its values' exponents are from the unit of the sums
+    auto step = [&](int t) {
+      blocks.step(t);
+#pragma unroll
+      for (int k = 0; k < 4; k++) {
+        pages[k] = __shfl_sync(0xffffffffu, blocks.page, (t & 7) * 4 + k);
+        shift[k] = pages[k] >= 0 ? __shfl_sync(0xffffffffu, blocks.ve, (t & 7) * 4 + k) - blocks.unit : 0;
+      }
+    };
+    if (tiles > 0) {
+      step(0);
+      ask(0, codes[0], p.k_cache);
+      ask(0, codes[1], p.v_cache);
+    }
+    for (int t = 0; t < tiles; t++) {
+      const int stage = t & 1;
+      const uint32_t parity = (uint32_t)(t >> 1) & 1u;
+      int now[4];
+#pragma unroll
+      for (int k = 0; k < 4; k++) now[k] = shift[k];
+      if (t + 1 < tiles) step(t + 1);
+      ok = prompt_wait(k_empty + 8 * stage, parity ^ 1u);
+      if (!ok) break;
+      put(codes[0], base + L::k + stage * L::tile_bytes, false, now);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      mbar_arrive(k_full + 8 * stage);
+      if (t + 1 < tiles) ask(t + 1, codes[0], p.k_cache);
+      ok = prompt_wait(v_empty + 8 * stage, parity ^ 1u);
+      if (!ok) break;
+      put(codes[1], base + L::v + stage * L::tile_bytes, true, now);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      mbar_arrive(v_full + 8 * stage);
+      if (t + 1 < tiles) ask(t + 1, codes[1], p.v_cache);
+    }
+  } else {
+    // ---------------------------------------------------------------- issuers, one a row tile
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    const int half = warp - 12;
+    if (half < halves) {
+      const uint32_t elected = elect_one() ? 1u : 0u;
+      // 128-byte swizzle, eight rows 1024 bytes; values: 64 elements and 64 keys on, a block on
+      const uint32_t desc_hi = (1024u >> 4) | (1u << 14) | (2u << 29);
+      const uint32_t q0 = (base + L::q + half * L::tile_bytes) >> 4 | 1u << 16;
+      const uint32_t k0 = (base + L::k) >> 4 | 1u << 16, v0 = (base + L::v) >> 4 | (uint32_t)(BLOCK >> 4) << 16;
+      const uint32_t idesc_s = (1u << 4) | (uint32_t)(kPromptKeys >> 3) << 17 | 8u << 24;
+      const uint32_t idesc_o = (1u << 4) | 1u << 16 | (uint32_t)(DIM >> 3) << 17 | 8u << 24;
+      const uint32_t at_s = kS + 128u * half, at_o = kO + (uint32_t)(DIM * half);
+      auto scores = [&](int t) {
+        const int stage = t & 1;
+        ok = prompt_wait(k_full + 8 * stage, (uint32_t)(t >> 1) & 1u);
+        if (!ok) return;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t kb = k0 + (uint32_t)(stage * (L::tile_bytes >> 4));
+#pragma unroll
+        for (int x = 0; x < DIM / 16; x++) {
+          const uint32_t in = (uint32_t)((x >> 2) * (BLOCK >> 4) + (x & 3) * 2);
+          umma_ss(elected, at_s, q0 + in, kb + in, desc_hi, idesc_s, x > 0 ? 1u : 0u);
+        }
+        umma_commit(elected, s_full + 8 * half);
+        umma_commit(elected, k_empty + 8 * stage);
+      };
+      if (tiles > 0) scores(0);
+      for (int t = 0; t < tiles && ok; t++) {
+        const int stage = t & 1;
+        ok = prompt_wait(v_full + 8 * stage, (uint32_t)(t >> 1) & 1u) && prompt_wait(p_full + 8 * half, t & 1);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t vb = v0 + (uint32_t)(stage * (L::tile_bytes >> 4));
+#pragma unroll
+        for (int x = 0; x < kPromptKeys / 16; x++)
+          umma_ts(elected, at_o, at_s + 8u * x, vb + 128u * x, desc_hi, idesc_o, t > 0 || x > 0 ? 1u : 0u);
+        umma_commit(elected, o_done + 8 * half);
+        umma_commit(elected, v_empty + 8 * stage);
+        if (t + 1 < tiles) {
+          // the next scores take the weights' place when those have been multiplied
+          ok = prompt_wait(o_done + 8 * half, t & 1);
+          if (ok) scores(t + 1);
+        }
+      }
+      // nothing of this warp is at work any more when tensor and shared memory are given back
+      umma_commit(elected, drained + 8 * half);
+      __syncwarp();
+      prompt_wait(drained + 8 * half, 0);
+    }
+  }
+  if (!ok && lane == 0) atomicExch(p.status, warp < 8 ? 3 : warp < 12 ? 4 : 5);
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (warp == 15) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(0), "r"(512) : "memory");
+  }
+}
+
+}  // namespace rcp
