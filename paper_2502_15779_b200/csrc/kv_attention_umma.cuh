@@ -68,6 +68,25 @@ __device__ __forceinline__ void umma_ts(uint32_t elected, uint32_t d, uint32_t a
 
 __device__ __forceinline__ bool prompt_wait(uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, kPromptPolls); }
 
+// two fp32 numbers at a time
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
 // Pages and scales of a sequence's keys in units of 32, one unit a lane, 32 units (eight tiles) at a time; the next 32 are asked for ahead.
 struct PromptBlocks {
   const KvSeqs* s;
@@ -211,27 +230,28 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
         ok = prompt_wait(s_full + 8 * half, t & 1);
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        uint32_t s[4][32];
+        // The scores are read twice, 32 at a time, the next 32 on their way: all 128 at once took so many registers that some went to local
+        // memory (638 us instead of the 5xx of this form at three prompts of 2000 tokens at most).
+        const bool partial = !some || (t + 1) * kPromptKeys > least;   // keys that some row of the warp does not see, or that are not there
+        uint32_t s[2][32];
+        auto hide = [&](uint32_t (&x)[32], int k) {
+          const int left = __shfl_sync(0xffffffffu, blocks.page, (t & 7) * 4 + k) >= 0 ? lim - t * kPromptKeys - 32 * k : 0;
 #pragma unroll
-        for (int k = 0; k < 4; k++) tmem_ld32(at_s + 32u * k, s[k]);
-        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-        if (!some || (t + 1) * kPromptKeys > least) {   // keys that some row of the warp does not see, or that are not there
-#pragma unroll
-          for (int k = 0; k < 4; k++) {
-            const bool there = __shfl_sync(0xffffffffu, blocks.page, (t & 7) * 4 + k) >= 0;
-            const int left = there ? lim - t * kPromptKeys - 32 * k : 0;
-#pragma unroll
-            for (int x = 0; x < 32; x++)
-              if (x >= left) s[k][x] = 0xFF800000u;
-          }
-        }
+          for (int n = 0; n < 32; n++)
+            if (n >= left) x[n] = 0xFF800000u;
+        };
         float top = -INFINITY;
+        tmem_ld32(at_s, s[0]);
 #pragma unroll
         for (int k = 0; k < 4; k++) {
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          tmem_ld32(at_s + 32u * ((k + 1) & 3), s[(k + 1) & 1]);   // (behind the last the first again, for the second reading)
+          uint32_t(&x)[32] = s[k & 1];
+          if (partial) hide(x, k);
           float a[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int x = 0; x < 32; x++) a[x & 3] = fmaxf(a[x & 3], __uint_as_float(s[k][x]));
-          top = fmaxf(top, fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])) * c[k]);
+          for (int n = 0; n < 16; n++) a[n & 3] = max3(a[n & 3], __uint_as_float(x[2 * n]), __uint_as_float(x[2 * n + 1]));
+          top = fmaxf(top, max3(fmaxf(a[0], a[1]), a[2], a[3]) * c[k]);
         }
         if (__any_sync(0xffffffffu, top > m + kAttnSlack || grow != 0)) {
           const float mn = fmaxf(m, top), f = exp2_fast(m - mn);
@@ -252,21 +272,24 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
           }
         }
         const float ref = m - kAttnLift;
-        float sum[4] = {};
+        float2 sum[2] = {};
 #pragma unroll
         for (int k = 0; k < 4; k++) {
           uint32_t w[16];
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          if (k < 3) tmem_ld32(at_s + 32u * (k + 1), s[(k + 1) & 1]);
+          if (partial) hide(s[k & 1], k);
 #pragma unroll
           for (int x = 0; x < 16; x++) {
-            const float e0 = exp2_fast(fmaf(__uint_as_float(s[k][2 * x]), c[k], -ref)), e1 = exp2_fast(fmaf(__uint_as_float(s[k][2 * x + 1]), c[k], -ref));
-            const __half2 h = __floats2half2_rn(e0, e1);
+            const float2 y = fma2(make_float2(__uint_as_float(s[k & 1][2 * x]), __uint_as_float(s[k & 1][2 * x + 1])), make_float2(c[k], c[k]), make_float2(-ref, -ref));
+            const float2 e = make_float2(exp2_fast(y.x), exp2_fast(y.y));
+            const __half2 h = __float22half2_rn(e);
             w[x] = *reinterpret_cast<const uint32_t*>(&h);
-            sum[(2 * x) & 3] += e0;
-            sum[(2 * x + 1) & 3] += e1;
+            sum[x & 1] = add2(sum[x & 1], e);
           }
           tmem_st16(at_s + 16u * k, w);
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         mbar_arrive(p_full + 8 * half);
@@ -302,64 +325,64 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
   } else if (warp < 12) {
     // ---------------------------------------------------------------- converters
     asm volatile("setmaxnreg.dec.sync.aligned.u32 112;");
-    constexpr int PIECES = DIM / 16, COPIES = PIECES;   // 16-byte pieces of codes: of a row, and of a thread (128 rows x PIECES / 128 threads)
-    const int me = tid - 256;
+    // A thread has row `me / 4` of each unit of 32 keys and a quarter of each of its 64-element blocks, 16 codes: 64 bytes of a row to four
+    // lanes, and no two lanes of eight that store together in the same banks (rows side by side differ in the swizzle).
+    constexpr int BLOCKS = DIM / 64, COPIES = 4 * BLOCKS;
+    const int me = tid - 256, row = me >> 2, quarter = me & 3;
     blocks.start();
     uint4 codes[2][COPIES];   // keys, values: asked for a tile ahead
-    int pages[4];
-    auto ask = [&](int t, uint4 (&to)[COPIES], const uint8_t* cache) {
+    long long from[4];        // the row's place in the cache, below zero: none
+    auto ask = [&](uint4 (&to)[COPIES], const uint8_t* cache) {
 #pragma unroll
-      for (int k = 0; k < COPIES; k++) {
-        const int n = me + 128 * k, row = n / PIECES, piece = n % PIECES, j = t * kPromptKeys + row;
-        // the row's unit of 32 keys does not depend on the thread: 128 / PIECES rows a step
-        const int pg = pages[k * (128 / PIECES) >> 5];
-        to[k] = make_uint4(0, 0, 0, 0);
-        if (pg >= 0 && j < sq.end)
-          to[k] = __ldcg(reinterpret_cast<const uint4*>(cache + (((long long)pg * p.kv_heads + kv) * p.s.page + (j & (p.s.page - 1))) * DIM + 16 * piece));
-      }
-    };
-    auto put = [&](const uint4 (&from)[COPIES], uint32_t dst, bool values, const int (&shift)[4]) {
+      for (int u = 0; u < 4; u++)
 #pragma unroll
-      for (int k = 0; k < COPIES; k++) {
-        const int n = me + 128 * k, row = n / PIECES, piece = n % PIECES;
-        uint32_t h[8];
-        e4m3_halves(from[k].x, h[0], h[1]);
-        e4m3_halves(from[k].y, h[2], h[3]);
-        e4m3_halves(from[k].z, h[4], h[5]);
-        e4m3_halves(from[k].w, h[6], h[7]);
-        if (values) {
-          const __half2 f = __float2half2_rn(kv_pow2(min(max(shift[k * (128 / PIECES) >> 5], -30), 7)));
-#pragma unroll
-          for (int x = 0; x < 8; x++) {
-            const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&h[x]), f);
-            h[x] = *reinterpret_cast<const uint32_t*>(&y);
-          }
+        for (int k = 0; k < BLOCKS; k++) {
+          to[u * BLOCKS + k] = make_uint4(0, 0, 0, 0);
+          if (from[u] >= 0) to[u * BLOCKS + k] = __ldcg(reinterpret_cast<const uint4*>(cache + from[u] + 64 * k));
         }
-        // 16 elements are two pieces of 16 bytes; the second block's threads begin with the second one, other banks than the first block's
-        const uint32_t at = dst + (uint32_t)((piece >> 2) * BLOCK + row * 128);
-        const uint32_t c = (uint32_t)((piece & 3) * 2), odd = (uint32_t)(piece >> 2) & 1u, r7 = (uint32_t)row & 7u;
-        const uint4 first = odd ? make_uint4(h[4], h[5], h[6], h[7]) : make_uint4(h[0], h[1], h[2], h[3]);
-        const uint4 second = odd ? make_uint4(h[0], h[1], h[2], h[3]) : make_uint4(h[4], h[5], h[6], h[7]);
-        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at + (((c + odd) ^ r7) << 4)), "r"(first.x), "r"(first.y), "r"(first.z), "r"(first.w)
-                     : "memory");
-        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at + (((c + 1 - odd) ^ r7) << 4)), "r"(second.x), "r"(second.y), "r"(second.z), "r"(second.w)
-                     : "memory");
+    };
+    const uint32_t to0 = (uint32_t)(row * 128) + (((uint32_t)(2 * quarter) ^ ((uint32_t)row & 7u)) << 4);
+    auto put = [&](const uint4 (&codes)[COPIES], uint32_t dst, bool values, const int (&shift)[4]) {
+#pragma unroll
+      for (int u = 0; u < 4; u++) {
+        const __half2 f = __float2half2_rn(kv_pow2(min(max(shift[u], -30), 7)));
+#pragma unroll
+        for (int k = 0; k < BLOCKS; k++) {
+          const uint4 c = codes[u * BLOCKS + k];
+          uint32_t h[8];
+          e4m3_halves(c.x, h[0], h[1]);
+          e4m3_halves(c.y, h[2], h[3]);
+          e4m3_halves(c.z, h[4], h[5]);
+          e4m3_halves(c.w, h[6], h[7]);
+          if (values) {
+#pragma unroll
+            for (int x = 0; x < 8; x++) {
+              const __half2 y = __hmul2(*reinterpret_cast<const __half2*>(&h[x]), f);
+              h[x] = *reinterpret_cast<const uint32_t*>(&y);
+            }
+          }
+          const uint32_t at = dst + to0 + (uint32_t)(k * BLOCK + u * 32 * 128);
+          asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
+          asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at ^ 16u), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
+        }
       }
     };
     int shift[4];
-    // pages of tile t, and how far its values' exponents are from the unit of the sums
+    // where the thread's rows of tile t are, and how far the values' exponents are from the unit of the sums
     auto step = [&](int t) {
       blocks.step(t);
 #pragma unroll
       for (int k = 0; k < 4; k++) {
-        pages[k] = __shfl_sync(0xffffffffu, blocks.page, (t & 7) * 4 + k);
-        shift[k] = pages[k] >= 0 ? __shfl_sync(0xffffffffu, blocks.ve, (t & 7) * 4 + k) - blocks.unit : 0;
+        const int page = __shfl_sync(0xffffffffu, blocks.page, (t & 7) * 4 + k), ve = __shfl_sync(0xffffffffu, blocks.ve, (t & 7) * 4 + k);
+        const int j = t * kPromptKeys + 32 * k + row;
+        shift[k] = page >= 0 ? ve - blocks.unit : 0;
+        from[k] = page >= 0 && j < sq.end ? (((long long)page * p.kv_heads + kv) * p.s.page + (j & (p.s.page - 1))) * DIM + 16 * quarter : -1;
       }
     };
     if (tiles > 0) {
       step(0);
-      ask(0, codes[0], p.k_cache);
-      ask(0, codes[1], p.v_cache);
+      ask(codes[0], p.k_cache);
+      ask(codes[1], p.v_cache);
     }
     for (int t = 0; t < tiles; t++) {
       const int stage = t & 1;
@@ -373,13 +396,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
       put(codes[0], base + L::k + stage * L::tile_bytes, false, now);
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       mbar_arrive(k_full + 8 * stage);
-      if (t + 1 < tiles) ask(t + 1, codes[0], p.k_cache);
+      if (t + 1 < tiles) ask(codes[0], p.k_cache);
       ok = prompt_wait(v_empty + 8 * stage, parity ^ 1u);
       if (!ok) break;
       put(codes[1], base + L::v + stage * L::tile_bytes, true, now);
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       mbar_arrive(v_full + 8 * stage);
-      if (t + 1 < tiles) ask(t + 1, codes[1], p.v_cache);
+      if (t + 1 < tiles) ask(codes[1], p.v_cache);
     }
   } else {
     // ---------------------------------------------------------------- issuers, one a row tile
