@@ -18,15 +18,15 @@
 
 namespace rcp {
 
-constexpr int kPromptThreads = 512, kPromptRows = 256, kPromptKeys = 128;
+constexpr int kPromptThreads = 512, kPromptRows = 256, kPromptKeys = 64, kPromptStages = 4;
 constexpr int kAttnFewRows = 64;   // sequences with no more rows than that go to kv_attention_split_kernel
 
 constexpr uint32_t kPromptPolls = 1u << 18;   // a wait of this kernel is a few microseconds
 
 template <int DIM>
 struct PromptLayout {
-  static constexpr int tile_bytes = kPromptKeys * DIM * 2;   // 128 rows in fp16: blocks of 64 elements, 128 bytes a row each
-  static constexpr int q = 0, k = 2 * tile_bytes, v = k + 2 * tile_bytes, bars = v + 2 * tile_bytes;
+  static constexpr int q_bytes = 128 * DIM * 2, tile_bytes = kPromptKeys * DIM * 2;   // fp16, in blocks of 64 elements: 128 bytes a row
+  static constexpr int q = 0, k = 2 * q_bytes, v = k + kPromptStages * tile_bytes, bars = v + kPromptStages * tile_bytes;
   static constexpr int bytes = bars + 256 + 1024;            // the swizzle wants 1024-byte alignment
 };
 
@@ -87,7 +87,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-// Pages and scales of a sequence's keys in units of 32, one unit a lane, 32 units (eight tiles) at a time; the next 32 are asked for ahead.
+// Pages and scales of a sequence's keys in units of 32, one unit a lane, 32 units (sixteen tiles) at a time; the next 32 are asked for ahead.
 struct PromptBlocks {
   const KvSeqs* s;
   const int32_t* row;                 // the sequence's row of the table
@@ -114,13 +114,12 @@ struct PromptBlocks {
   }
   // to be called for every tile in turn; returns by how many powers of two the sums' unit grows with it (0 as a rule)
   __device__ __forceinline__ int step(int tile) {
-    if ((tile & 7) == 0) {
+    if ((tile & 15) == 0) {
       page = next_page; ks = next_ks; ve = next_ve;
-      next_page = find((tile + 8) * 4 + lane);
+      next_page = find((tile + 16) * 2 + lane);
     }
-    if ((tile & 7) == 4) scales(next_page, next_ks, next_ve);
-    const int at = (tile & 7) * 4;
-    const int top = __reduce_max_sync(0xffffffffu, lane >= at && lane < at + 4 ? ve : INT_MIN);
+    if ((tile & 15) == 8) scales(next_page, next_ks, next_ve);
+    const int at = (tile & 15) * 2, a = __shfl_sync(0xffffffffu, ve, at), b = __shfl_sync(0xffffffffu, ve, at + 1), top = max(a, b);
     if (top == INT_MIN) return 0;                       // no keys in this tile
     if (unit != INT_MIN && top - unit <= 7 && top - unit >= -11) return 0;
     const int grow = unit == INT_MIN ? 0 : top + 4 - unit;
@@ -132,7 +131,7 @@ struct PromptBlocks {
 template <int DIM>
 __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(const AttnParams p) {
   using L = PromptLayout<DIM>;
-  constexpr int BLOCK = kPromptKeys * 128;   // bytes of a 64-element block of 128 rows
+  constexpr int BLOCK_Q = 128 * 128, BLOCK = kPromptKeys * 128;   // bytes of a 64-element block of 128 queries, of a tile's keys
   extern __shared__ uint8_t prompt_raw[];
   __shared__ uint32_t s_tmem;
   const uint32_t raw = smem_u32(prompt_raw), base = (raw + 1023u) & ~1023u;
@@ -162,15 +161,20 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
   const int halves = rows > 128 ? 2 : 1;
 
   const uint32_t bar = base + L::bars;
-  const uint32_t k_full = bar, k_empty = bar + 16, v_full = bar + 32, v_empty = bar + 48;   // two stages each
-  const uint32_t s_full = bar + 64, p_full = bar + 80, o_done = bar + 96, drained = bar + 112;   // one for each row tile
+  constexpr uint32_t STAGES = kPromptStages;
+  const uint32_t k_full = bar, k_empty = k_full + 8 * STAGES, v_full = k_empty + 8 * STAGES, v_empty = v_full + 8 * STAGES;
+  const uint32_t s_full = v_empty + 8 * STAGES;                                      // [row tile][buffer]
+  const uint32_t p_full = s_full + 32, o_done = p_full + 16, drained = o_done + 16;   // [row tile]
   if (tid == 0) {
-    for (int i = 0; i < 2; i++) {
+    for (uint32_t i = 0; i < STAGES; i++) {
       mbar_init(k_full + 8 * i, 128);
       mbar_init(k_empty + 8 * i, halves);
       mbar_init(v_full + 8 * i, 128);
       mbar_init(v_empty + 8 * i, halves);
-      mbar_init(s_full + 8 * i, 1);
+    }
+    for (int i = 0; i < 2; i++) {
+      mbar_init(s_full + 16 * i, 1);
+      mbar_init(s_full + 16 * i + 8, 1);
       mbar_init(p_full + 8 * i, 128);
       mbar_init(o_done + 8 * i, 1);
       mbar_init(drained + 8 * i, 1);
@@ -187,7 +191,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
     uint4 v = make_uint4(0, 0, 0, 0);
     if (row < rows)
       v = *reinterpret_cast<const uint4*>(p.q + (long long)(sq.t0 + i) * p.q_stride + (long long)(kv * p.group + r - i * p.group) * DIM + 8 * c);
-    *reinterpret_cast<uint4*>(gen + L::q + (row >> 7) * L::tile_bytes + (c >> 3) * BLOCK + (row & 127) * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
+    *reinterpret_cast<uint4*>(gen + L::q + (row >> 7) * L::q_bytes + (c >> 3) * BLOCK_Q + (row & 127) * 128 + (((c & 7) ^ (row & 7)) << 4)) = v;
   }
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -219,47 +223,48 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
       blocks.start();
       for (int t = 0; t < tiles; t++) {
         const int grow = blocks.step(t);
-        float c[4];
+        float c[2];
         bool some = true;
 #pragma unroll
-        for (int k = 0; k < 4; k++) {
-          const int from = (t & 7) * 4 + k;
+        for (int k = 0; k < 2; k++) {
+          const int from = (t & 15) * 2 + k;
           c[k] = fmaxf(__shfl_sync(0xffffffffu, blocks.ks, from) * p.scale_log2, 1e-37f);   // above zero: a score of -inf stays one
           some = some && __shfl_sync(0xffffffffu, blocks.page, from) >= 0;
         }
-        ok = prompt_wait(s_full + 8 * half, t & 1);
+        const uint32_t at = at_s + 64u * (t & 1);
+        ok = prompt_wait(s_full + 16 * half + 8 * (t & 1), (uint32_t)(t >> 1) & 1u);
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        // The scores are read twice, 32 at a time, the next 32 on their way: all 128 at once took so many registers that some went to local
-        // memory (638 us instead of the 5xx of this form at three prompts of 2000 tokens at most).
-        const bool partial = !some || (t + 1) * kPromptKeys > least;   // keys that some row of the warp does not see, or that are not there
         uint32_t s[2][32];
-        auto hide = [&](uint32_t (&x)[32], int k) {
-          const int left = __shfl_sync(0xffffffffu, blocks.page, (t & 7) * 4 + k) >= 0 ? lim - t * kPromptKeys - 32 * k : 0;
+        tmem_ld32(at, s[0]);
+        tmem_ld32(at + 32u, s[1]);
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        if (!some || (t + 1) * kPromptKeys > least) {   // keys that some row of the warp does not see, or that are not there
 #pragma unroll
-          for (int n = 0; n < 32; n++)
-            if (n >= left) x[n] = 0xFF800000u;
-        };
+          for (int k = 0; k < 2; k++) {
+            const int left = __shfl_sync(0xffffffffu, blocks.page, (t & 15) * 2 + k) >= 0 ? lim - t * kPromptKeys - 32 * k : 0;
+#pragma unroll
+            for (int x = 0; x < 32; x++)
+              if (x >= left) s[k][x] = 0xFF800000u;
+          }
+        }
         float top = -INFINITY;
-        tmem_ld32(at_s, s[0]);
 #pragma unroll
-        for (int k = 0; k < 4; k++) {
-          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-          tmem_ld32(at_s + 32u * ((k + 1) & 3), s[(k + 1) & 1]);   // (behind the last the first again, for the second reading)
-          uint32_t(&x)[32] = s[k & 1];
-          if (partial) hide(x, k);
+        for (int k = 0; k < 2; k++) {
           float a[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int n = 0; n < 16; n++) a[n & 3] = max3(a[n & 3], __uint_as_float(x[2 * n]), __uint_as_float(x[2 * n + 1]));
+          for (int x = 0; x < 16; x++) a[x & 3] = max3(a[x & 3], __uint_as_float(s[k][2 * x]), __uint_as_float(s[k][2 * x + 1]));
           top = fmaxf(top, max3(fmaxf(a[0], a[1]), a[2], a[3]) * c[k]);
         }
         if (__any_sync(0xffffffffu, top > m + kAttnSlack || grow != 0)) {
           const float mn = fmaxf(m, top), f = exp2_fast(m - mn);
           m = mn;
           l *= f;
-          // (the product into O of the tile in front is done: the scores of this one were asked for behind it)
           const float fu = f * kv_pow2(min(max(-grow, -100), 100));
           if (t > 0) {
+            ok = prompt_wait(o_done + 8 * half, (t - 1) & 1);   // the product of the tile in front is in the sums
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
             for (int d = 0; d < DIM / 32; d++) {
               uint32_t o[32];
@@ -274,26 +279,25 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
         const float ref = m - kAttnLift;
         float2 sum[2] = {};
 #pragma unroll
-        for (int k = 0; k < 4; k++) {
+        for (int k = 0; k < 2; k++) {
           uint32_t w[16];
-          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-          if (k < 3) tmem_ld32(at_s + 32u * (k + 1), s[(k + 1) & 1]);
-          if (partial) hide(s[k & 1], k);
 #pragma unroll
           for (int x = 0; x < 16; x++) {
-            const float2 y = fma2(make_float2(__uint_as_float(s[k & 1][2 * x]), __uint_as_float(s[k & 1][2 * x + 1])), make_float2(c[k], c[k]), make_float2(-ref, -ref));
+            const float2 y = fma2(make_float2(__uint_as_float(s[k][2 * x]), __uint_as_float(s[k][2 * x + 1])), make_float2(c[k], c[k]), make_float2(-ref, -ref));
             const float2 e = make_float2(exp2_fast(y.x), exp2_fast(y.y));
             const __half2 h = __float22half2_rn(e);
             w[x] = *reinterpret_cast<const uint32_t*>(&h);
             sum[x & 1] = add2(sum[x & 1], e);
           }
-          tmem_st16(at_s + 16u * k, w);
+          tmem_st16(at + 16u * k, w);
         }
         l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         mbar_arrive(p_full + 8 * half);
       }
+      // (one after the other: a wait by parity is good for the phase behind one that is known to be over)
+      if (ok && tiles > 1) ok = prompt_wait(o_done + 8 * half, (tiles - 2) & 1);
       if (ok && tiles > 0) ok = prompt_wait(o_done + 8 * half, (tiles - 1) & 1);
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       if (ok) {
@@ -327,14 +331,14 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
     asm volatile("setmaxnreg.dec.sync.aligned.u32 112;");
     // A thread has row `me / 4` of each unit of 32 keys and a quarter of each of its 64-element blocks, 16 codes: 64 bytes of a row to four
     // lanes, and no two lanes of eight that store together in the same banks (rows side by side differ in the swizzle).
-    constexpr int BLOCKS = DIM / 64, COPIES = 4 * BLOCKS;
+    constexpr int BLOCKS = DIM / 64, UNITS = kPromptKeys / 32, COPIES = UNITS * BLOCKS;
     const int me = tid - 256, row = me >> 2, quarter = me & 3;
     blocks.start();
     uint4 codes[2][COPIES];   // keys, values: asked for a tile ahead
-    long long from[4];        // the row's place in the cache, below zero: none
+    long long from[UNITS];    // the row's place in the cache, below zero: none
     auto ask = [&](uint4 (&to)[COPIES], const uint8_t* cache) {
 #pragma unroll
-      for (int u = 0; u < 4; u++)
+      for (int u = 0; u < UNITS; u++)
 #pragma unroll
         for (int k = 0; k < BLOCKS; k++) {
           to[u * BLOCKS + k] = make_uint4(0, 0, 0, 0);
@@ -342,9 +346,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
         }
     };
     const uint32_t to0 = (uint32_t)(row * 128) + (((uint32_t)(2 * quarter) ^ ((uint32_t)row & 7u)) << 4);
-    auto put = [&](const uint4 (&codes)[COPIES], uint32_t dst, bool values, const int (&shift)[4]) {
+    auto put = [&](const uint4 (&codes)[COPIES], uint32_t dst, bool values, const int (&shift)[UNITS]) {
 #pragma unroll
-      for (int u = 0; u < 4; u++) {
+      for (int u = 0; u < UNITS; u++) {
         const __half2 f = __float2half2_rn(kv_pow2(min(max(shift[u], -30), 7)));
 #pragma unroll
         for (int k = 0; k < BLOCKS; k++) {
@@ -367,13 +371,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
         }
       }
     };
-    int shift[4];
+    int shift[UNITS];
     // where the thread's rows of tile t are, and how far the values' exponents are from the unit of the sums
     auto step = [&](int t) {
       blocks.step(t);
 #pragma unroll
-      for (int k = 0; k < 4; k++) {
-        const int page = __shfl_sync(0xffffffffu, blocks.page, (t & 7) * 4 + k), ve = __shfl_sync(0xffffffffu, blocks.ve, (t & 7) * 4 + k);
+      for (int k = 0; k < UNITS; k++) {
+        const int page = __shfl_sync(0xffffffffu, blocks.page, (t & 15) * 2 + k), ve = __shfl_sync(0xffffffffu, blocks.ve, (t & 15) * 2 + k);
         const int j = t * kPromptKeys + 32 * k + row;
         shift[k] = page >= 0 ? ve - blocks.unit : 0;
         from[k] = page >= 0 && j < sq.end ? (((long long)page * p.kv_heads + kv) * p.s.page + (j & (p.s.page - 1))) * DIM + 16 * quarter : -1;
@@ -385,11 +389,11 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
       ask(codes[1], p.v_cache);
     }
     for (int t = 0; t < tiles; t++) {
-      const int stage = t & 1;
-      const uint32_t parity = (uint32_t)(t >> 1) & 1u;
-      int now[4];
+      const int stage = t % kPromptStages;
+      const uint32_t parity = (uint32_t)(t / kPromptStages) & 1u;
+      int now[UNITS];
 #pragma unroll
-      for (int k = 0; k < 4; k++) now[k] = shift[k];
+      for (int k = 0; k < UNITS; k++) now[k] = shift[k];
       if (t + 1 < tiles) step(t + 1);
       ok = prompt_wait(k_empty + 8 * stage, parity ^ 1u);
       if (!ok) break;
@@ -412,42 +416,42 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
       const uint32_t elected = elect_one() ? 1u : 0u;
       // 128-byte swizzle, eight rows 1024 bytes; values: 64 elements and 64 keys on, a block on
       const uint32_t desc_hi = (1024u >> 4) | (1u << 14) | (2u << 29);
-      const uint32_t q0 = (base + L::q + half * L::tile_bytes) >> 4 | 1u << 16;
+      const uint32_t q0 = (base + L::q + half * L::q_bytes) >> 4 | 1u << 16;
       const uint32_t k0 = (base + L::k) >> 4 | 1u << 16, v0 = (base + L::v) >> 4 | (uint32_t)(BLOCK >> 4) << 16;
       const uint32_t idesc_s = (1u << 4) | (uint32_t)(kPromptKeys >> 3) << 17 | 8u << 24;
       const uint32_t idesc_o = (1u << 4) | 1u << 16 | (uint32_t)(DIM >> 3) << 17 | 8u << 24;
       const uint32_t at_s = kS + 128u * half, at_o = kO + (uint32_t)(DIM * half);
       auto scores = [&](int t) {
-        const int stage = t & 1;
-        ok = prompt_wait(k_full + 8 * stage, (uint32_t)(t >> 1) & 1u);
+        const int stage = t % kPromptStages;
+        ok = prompt_wait(k_full + 8 * stage, (uint32_t)(t / kPromptStages) & 1u);
         if (!ok) return;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t kb = k0 + (uint32_t)(stage * (L::tile_bytes >> 4));
 #pragma unroll
-        for (int x = 0; x < DIM / 16; x++) {
-          const uint32_t in = (uint32_t)((x >> 2) * (BLOCK >> 4) + (x & 3) * 2);
-          umma_ss(elected, at_s, q0 + in, kb + in, desc_hi, idesc_s, x > 0 ? 1u : 0u);
-        }
-        umma_commit(elected, s_full + 8 * half);
+        for (int x = 0; x < DIM / 16; x++)
+          umma_ss(elected, at_s + 64u * (t & 1), q0 + (uint32_t)((x >> 2) * (BLOCK_Q >> 4) + (x & 3) * 2),
+                  kb + (uint32_t)((x >> 2) * (BLOCK >> 4) + (x & 3) * 2), desc_hi, idesc_s, x > 0 ? 1u : 0u);
+        umma_commit(elected, s_full + 16 * half + 8 * (t & 1));
         umma_commit(elected, k_empty + 8 * stage);
       };
       if (tiles > 0) scores(0);
       for (int t = 0; t < tiles && ok; t++) {
-        const int stage = t & 1;
-        ok = prompt_wait(v_full + 8 * stage, (uint32_t)(t >> 1) & 1u) && prompt_wait(p_full + 8 * half, t & 1);
+        // the next scores, while the softmax works on these: they take the place of weights that have been multiplied
+        if (t + 1 < tiles) {
+          if (t > 0) ok = prompt_wait(o_done + 8 * half, (t - 1) & 1);
+          if (ok) scores(t + 1);
+          if (!ok) break;
+        }
+        const int stage = t % kPromptStages;
+        ok = prompt_wait(v_full + 8 * stage, (uint32_t)(t / kPromptStages) & 1u) && prompt_wait(p_full + 8 * half, t & 1);
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t vb = v0 + (uint32_t)(stage * (L::tile_bytes >> 4));
 #pragma unroll
         for (int x = 0; x < kPromptKeys / 16; x++)
-          umma_ts(elected, at_o, at_s + 8u * x, vb + 128u * x, desc_hi, idesc_o, t > 0 || x > 0 ? 1u : 0u);
+          umma_ts(elected, at_o, at_s + 64u * (t & 1) + 8u * x, vb + 128u * x, desc_hi, idesc_o, t > 0 || x > 0 ? 1u : 0u);
         umma_commit(elected, o_done + 8 * half);
         umma_commit(elected, v_empty + 8 * stage);
-        if (t + 1 < tiles) {
-          // the next scores take the weights' place when those have been multiplied
-          ok = prompt_wait(o_done + 8 * half, t & 1);
-          if (ok) scores(t + 1);
-        }
       }
       // nothing of this warp is at work any more when tensor and shared memory are given back
       umma_commit(elected, drained + 8 * half);
