@@ -114,25 +114,35 @@ int rcp_kv_append(const void* q_f16, int64_t q_stride, const void* k_f16, int64_
   p.v_cache = static_cast<uint8_t*>(v_cache);
   p.k_scale = k_scale; p.v_scale = v_scale;
   p.q_out = static_cast<__half*>(q_out_f16);
-  // candidates for blocks with new tokens: so many to each sequence, or by search over starts
-  const int64_t per = (p.s.max_new + page - 2) / page + 1, direct = per * seqs, found = tokens / page + 2 * (int64_t)seqs;
-  p.direct = direct <= found ? (int)per : 0;
-  p.candidates = (int)std::min(direct, found);
-  int64_t ctas = (int64_t)p.candidates * kv_heads * 2;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const bool one = p.s.max_new == 1;
+  const int threads = !one && page * dim > 8192 ? 256 : rcp::kAppendThreads, query_tokens = threads / (dim / 16);
+  int64_t ctas;
+  if (one) {
+    const int per_warp = 512 / dim;
+    ctas = p.candidates = (int)(((int64_t)seqs * ((2 * kv_heads + per_warp - 1) / per_warp) + 3) / 4);
+  } else {
+    // candidates for blocks with new tokens: so many to each sequence, or by search over starts
+    const int64_t per = (p.s.max_new + page - 2) / page + 1, direct = per * seqs, found = tokens / page + 2 * (int64_t)seqs;
+    p.direct = direct <= found ? (int)per : 0;
+    p.candidates = (int)std::min(direct, found);
+    ctas = (int64_t)p.candidates * kv_heads * 2;
+  }
   if (q_f16) {
-    p.query_tokens = rcp::kAppendThreads / (dim / 16);
-    p.query_splits = (heads + rcp::kQueryHeads - 1) / rcp::kQueryHeads;
-    ctas += (int64_t)((tokens + p.query_tokens - 1) / p.query_tokens) * p.query_splits;
+    // eight heads a thread, fewer where there would be too few CTAs to share the latency
+    const int64_t groups = (tokens + query_tokens - 1) / query_tokens;
+    int each = 8;
+    while (each > 1 && groups * ((heads + each - 1) / each) < 2 * sm_count()) each /= 2;
+    p.query_splits = (heads + each - 1) / each;
+    ctas += groups * p.query_splits;
   }
   if (ctas > INT_MAX) return RCP_ERR_LIMIT;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const dim3 grid((unsigned)ctas), block(rcp::kAppendThreads);
-  switch (page * dim / 16 / rcp::kAppendThreads) {
-    case 1: RCP_CUDA(launch_overlapped(rcp::kv_append_kernel<1>, grid, block, 0, st, p)); break;
-    case 2: RCP_CUDA(launch_overlapped(rcp::kv_append_kernel<2>, grid, block, 0, st, p)); break;
-    case 4: RCP_CUDA(launch_overlapped(rcp::kv_append_kernel<4>, grid, block, 0, st, p)); break;
-    default: RCP_CUDA(launch_overlapped(rcp::kv_append_kernel<8>, grid, block, 0, st, p)); break;
-  }
+  const dim3 grid((unsigned)ctas), block(threads);
+  if (one) RCP_CUDA(launch_overlapped(rcp::kv_append_one_kernel, grid, block, 0, st, p));
+  else if (threads == 256) RCP_CUDA(launch_overlapped(rcp::kv_append_kernel<4, 256>, grid, block, 0, st, p));
+  else if (page * dim == 8192) RCP_CUDA(launch_overlapped(rcp::kv_append_kernel<4, 128>, grid, block, 0, st, p));
+  else if (page * dim == 4096) RCP_CUDA(launch_overlapped(rcp::kv_append_kernel<2, 128>, grid, block, 0, st, p));
+  else RCP_CUDA(launch_overlapped(rcp::kv_append_kernel<1, 128>, grid, block, 0, st, p));
   return RCP_OK;
 }
 
