@@ -116,7 +116,7 @@ int rcp_kv_append(const void* q_f16, int64_t q_stride, const void* k_f16, int64_
   p.q_out = static_cast<__half*>(q_out_f16);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool one = p.s.max_new == 1;
-  const int threads = !one && page * dim > 8192 ? 256 : rcp::kAppendThreads, query_tokens = threads / (dim / 16);
+  const int threads = !one && page * dim > 4096 ? 256 : rcp::kAppendThreads, query_tokens = threads / (dim / 16);
   int64_t ctas;
   if (one) {
     const int per_warp = 512 / dim;
@@ -139,8 +139,8 @@ int rcp_kv_append(const void* q_f16, int64_t q_stride, const void* k_f16, int64_
   if (ctas > INT_MAX) return RCP_ERR_LIMIT;
   const dim3 grid((unsigned)ctas), block(threads);
   if (one) RCP_CUDA(launch_overlapped(rcp::kv_append_one_kernel, grid, block, 0, st, p));
-  else if (threads == 256) RCP_CUDA(launch_overlapped(rcp::kv_append_kernel<4, 256>, grid, block, 0, st, p));
-  else if (page * dim == 8192) RCP_CUDA(launch_overlapped(rcp::kv_append_kernel<4, 128>, grid, block, 0, st, p));
+  else if (page * dim == 16384) RCP_CUDA(launch_overlapped(rcp::kv_append_kernel<4, 256>, grid, block, 0, st, p));
+  else if (page * dim == 8192) RCP_CUDA(launch_overlapped(rcp::kv_append_kernel<2, 256>, grid, block, 0, st, p));
   else if (page * dim == 4096) RCP_CUDA(launch_overlapped(rcp::kv_append_kernel<2, 128>, grid, block, 0, st, p));
   else RCP_CUDA(launch_overlapped(rcp::kv_append_kernel<1, 128>, grid, block, 0, st, p));
   return RCP_OK;
