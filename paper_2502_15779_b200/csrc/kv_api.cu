@@ -68,6 +68,12 @@ int attn_split(const rcp::AttnParams& p, cudaStream_t st) {
   return RCP_OK;
 }
 
+// Rows of a sequence (new tokens x query heads of a key head) up to which the split kernel takes it: one row tile of it where the
+// prompt kernel's CTAs, one a key head and sequence, fill the GPU without a split along the keys, three otherwise. Measured, split against
+// prompt kernel, us, 8 key heads: 16 sequences x 32 rows x 4000 keys 69 : 25, x 64 rows 91 : 27; 8 x 48 x 8000 61 : 90; 4 x 64 x 4000
+// 36 : 60; 2 x 64 x 30000 78 : 314.
+int attn_few_rows(int seqs, int kv_heads) { return (int64_t)seqs * kv_heads >= 2 * sm_count() / 3 ? rcp::kAttnMaxRows : 64; }
+
 template <int DIM>
 int attn_prompt(const rcp::AttnParams& p, cudaStream_t st) {
   using L = rcp::PromptLayout<DIM>;
@@ -173,10 +179,12 @@ int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads,
   p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + rcp::kAttnPartsAt);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   int64_t rows = (int64_t)p.s.max_new * p.group;
-  if (rows > rcp::kAttnFewRows) {
+  const int few = attn_few_rows(seqs, kv_heads);
+  if (rows > few) {
+    p.few = seqs > 1 ? few : 0;
     const int rc2 = dim == 64 ? attn_prompt<64>(p, st) : attn_prompt<128>(p, st);
     if (rc2 != RCP_OK || seqs == 1) return rc2;
-    p.few = rows = rcp::kAttnFewRows;   // and the sequences with few rows
+    rows = few;   // and the sequences with few rows
   }
   const int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 3;
   if (dim == 64) return nt == 1 ? attn_split<64, 1>(p, st) : nt == 2 ? attn_split<64, 2>(p, st) : attn_split<64, 3>(p, st);

@@ -38,7 +38,7 @@ struct AttnParams {
   const float *k_scale, *v_scale;
   __half* out;               // [tokens][heads][dim]
   int32_t* status;           // set when a bounded wait gives up
-  int few;                   // sequences with more rows than that are not this call's (0: all are)
+  int few;                   // sequences with more rows than that are the prompt kernel's, the others the split kernel's (0: one kernel has all)
   int32_t* arrived;          // [kAttnMaxCtas], zero between calls
   float* parts;              // [kAttnMaxCtas][2][rows][dim + 2]
 };
@@ -139,6 +139,12 @@ __device__ __forceinline__ __half* attn_row(const AttnParams& p, const KvSeq& sq
   return p.out + ((long long)(sq.t0 + i) * p.heads + (long long)(seg % p.kv_heads) * p.group + (r - i * p.group)) * DIM;
 }
 
+template <int E>
+__device__ __forceinline__ void attn_store(__half* to, const float (&acc)[E], float f) {
+#pragma unroll
+  for (int k = 0; k < E; k += 2) *reinterpret_cast<__half2*>(to + k) = __floats2half2_rn(acc[k] * f, acc[k + 1] * f);
+}
+
 // DIM: of a head; NT: columns of eight rows a row tile has
 template <int DIM, int NT>
 __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(const AttnParams p) {
@@ -153,61 +159,92 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
 
-  // tiles in front of each sequence, by a scan over the sequences
-  long long* const before = reinterpret_cast<long long*>(attn_shared);
-  constexpr int PER = RCP_KV_MAX_SEQS / (kAttnWarps * 32);
-  long long mine[PER], sum = 0;
-  const int per = (p.s.seqs + kAttnWarps * 32 - 1) / (kAttnWarps * 32);
-#pragma unroll
-  for (int i = 0; i < PER; i++) {
-    mine[i] = 0;
-    if (i < per && tid * per + i < p.s.seqs) {
-      AttnPlace at;
-      attn_sequence<ROWS>(p, tid * per + i, at);
-      mine[i] = (long long)at.segs * at.tiles;
-    }
-    sum += mine[i];
-  }
-  long long upto = sum;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const long long o = __shfl_up_sync(0xffffffffu, upto, d);
-    if (lane >= d) upto += o;
-  }
-  if (lane == 31) s_sum[warp] = upto;
-  __syncthreads();
-  long long total = 0, run = upto - sum;
-#pragma unroll
-  for (int w = 0; w < kAttnWarps; w++) {
-    if (w < warp) run += s_sum[w];
-    total += s_sum[w];
-  }
-#pragma unroll
-  for (int i = 0; i < PER; i++) {
-    if (i < per && tid * per + i < p.s.seqs) before[tid * per + i] = run;
-    run += mine[i];
-  }
-  __syncthreads();
-  // this CTA's tiles (as many CTAs as have one for each of their warps), and this warp's among them
-  const long long ctas = min((long long)gridDim.x, (total + kAttnWarps - 1) / kAttnWarps);
-  if ((long long)blockIdx.x >= ctas) return;
-  const long long c0 = total * blockIdx.x / ctas, c1 = total * (blockIdx.x + 1) / ctas;
-  const long long w0 = c0 + (c1 - c0) * warp / kAttnWarps;
-  const int todo = (int)min(c0 + (c1 - c0) * (warp + 1) / kAttnWarps - w0, (long long)INT_MAX);
+  // Tiles in front of each sequence, and where this warp's share of them begins. Up to 32 sequences every warp finds that out for itself, a
+  // sequence a lane; more are scanned by the CTA.
+  long long total, c0, c1, w0, ctas;
+  auto share = [&]() {   // of `total`: as many CTAs as have a tile for each of their warps
+    ctas = min((long long)gridDim.x, (total + kAttnWarps - 1) / kAttnWarps);
+    if ((long long)blockIdx.x >= ctas) return false;
+    c0 = total * blockIdx.x / ctas;
+    c1 = total * (blockIdx.x + 1) / ctas;
+    w0 = c0 + (c1 - c0) * warp / kAttnWarps;
+    return true;
+  };
   AttnPlace at{};
-  if (todo > 0) {
-    int lo = 0, hi = p.s.seqs;   // the last sequence with no more than w0 tiles in front: it has some itself
+  long long in = 0;   // the share's first tile in its sequence
+  if (p.s.seqs <= 32) {
+    if (lane < p.s.seqs) attn_sequence<ROWS>(p, lane, at);
+    const long long mine = (long long)at.segs * at.tiles;
+    long long upto = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long o = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += o;
+    }
+    total = __shfl_sync(0xffffffffu, upto, 31);
+    if (!share()) return;
+    // the last sequence with no more than w0 tiles in front of it (it has some itself, or there is nothing to do)
+    const int b = 31 - __clz((int)__ballot_sync(0xffffffffu, lane < p.s.seqs && upto - mine <= w0));
+    in = w0 - __shfl_sync(0xffffffffu, upto - mine, b);
+    at.b = b;
+    at.segs = __shfl_sync(0xffffffffu, at.segs, b);
+    at.tiles = __shfl_sync(0xffffffffu, at.tiles, b);
+    at.sq.t0 = __shfl_sync(0xffffffffu, at.sq.t0, b);
+    at.sq.n = __shfl_sync(0xffffffffu, at.sq.n, b);
+    at.sq.first = __shfl_sync(0xffffffffu, at.sq.first, b);
+    at.sq.end = __shfl_sync(0xffffffffu, at.sq.end, b);
+  } else {
+    long long* const before = reinterpret_cast<long long*>(attn_shared);
+    constexpr int PER = RCP_KV_MAX_SEQS / (kAttnWarps * 32);
+    long long mine[PER], sum = 0;
+    const int per = (p.s.seqs + kAttnWarps * 32 - 1) / (kAttnWarps * 32);
+#pragma unroll
+    for (int i = 0; i < PER; i++) {
+      mine[i] = 0;
+      if (i < per && tid * per + i < p.s.seqs) {
+        attn_sequence<ROWS>(p, tid * per + i, at);
+        mine[i] = (long long)at.segs * at.tiles;
+      }
+      sum += mine[i];
+    }
+    long long upto = sum;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long o = __shfl_up_sync(0xffffffffu, upto, d);
+      if (lane >= d) upto += o;
+    }
+    if (lane == 31) s_sum[warp] = upto;
+    __syncthreads();
+    long long run = upto - sum;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < kAttnWarps; w++) {
+      if (w < warp) run += s_sum[w];
+      total += s_sum[w];
+    }
+#pragma unroll
+    for (int i = 0; i < PER; i++) {
+      if (i < per && tid * per + i < p.s.seqs) before[tid * per + i] = run;
+      run += mine[i];
+    }
+    __syncthreads();
+    if (!share()) return;
+    int lo = 0, hi = p.s.seqs;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (before[mid] <= w0) lo = mid; else hi = mid;
     }
     attn_sequence<ROWS>(p, lo, at);
-    const long long in = w0 - before[lo];
+    in = w0 - before[lo];
+    __syncthreads();   // the list of tiles gives way to the rings
+  }
+  const int todo = (int)min(c0 + (c1 - c0) * (warp + 1) / kAttnWarps - w0, (long long)INT_MAX);
+  if (todo > 0) {
     at.seg = (int)(in / at.tiles);
     at.tile = (int)(in - (long long)at.seg * at.tiles);
   }
-  if (lane < 2) list[2 * warp + lane].tiles = 0;
-  __syncthreads();
+  if (lane < 2) list[2 * warp + lane].tiles = 0;   // (written again and read by this warp, then by all behind a barrier)
+  __syncwarp();
 
   if (todo > 0) {
     const uint32_t ring = base + (uint32_t)(warp * S * L::stage_bytes);
@@ -344,10 +381,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
       float s[2][NT][4];
 #pragma unroll
       for (int t = 0; t < 2; t++) {
-#pragma unroll
-        for (int n = 0; n < NT; n++)
-#pragma unroll
-          for (int e = 0; e < 4; e++) s[t][n][e] = 0.f;
+        constexpr int CHAINS = NT < 3 ? 2 : 1;   // products of 16 keys add to CHAINS sums in turn: a shorter chain, where registers allow
+        float part[CHAINS][NT][4] = {};
 #pragma unroll
         for (int c = 0; c < KSTEPS / 4; c++) {
           uint4 x[2];
@@ -364,9 +399,13 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
             e4m3_halves(w0[k], a0, a2);
             e4m3_halves(w1[k], a1, a3);
 #pragma unroll
-            for (int n = 0; n < NT; n++) mma16816(s[t][n], a0, a1, a2, a3, q[n][4 * c + k][0], q[n][4 * c + k][1]);
+            for (int n = 0; n < NT; n++) mma16816(part[k % CHAINS][n], a0, a1, a2, a3, q[n][4 * c + k][0], q[n][4 * c + k][1]);
           }
         }
+#pragma unroll
+        for (int n = 0; n < NT; n++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) s[t][n][e] = CHAINS == 2 ? part[0][n][e] + part[CHAINS - 1][n][e] : part[0][n][e];
       }
       const float c = there != 0.f ? fmaxf(ks * p.scale_log2, 1e-37f) : 1.f;   // above zero: a score of -inf stays one
       const int j0 = at.tile * kAttnTile;
@@ -488,29 +527,32 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
     const bool whole = tiles == head.of;
     const int slot = head.tile0 > 0 ? 0 : 1;   // of a segment that does not begin here the first slot, of one that does not end here the second
     float* const mine = p.parts + ((size_t)blockIdx.x * 2 + slot) * PART;
-    for (int x = tid; x < ROWS * DIM / 4; x += kAttnWarps * 32) {
-      const int row = x / (DIM / 4), d = x % (DIM / 4) * 4;
-      float top = kAttnNoMax, sum = 0.f, acc[4] = {};
-      for (int s = s0; s < s1; s++)
-        if (list[s].tiles) top = fmaxf(top, part_of(s)[ROWS * DIM + row]);
-      for (int s = s0; s < s1; s++)
-        if (list[s].tiles) {
-          const float* const from = part_of(s);
-          const float f = exp2f(from[ROWS * DIM + row] - top);
-          const float4 v = *reinterpret_cast<const float4*>(from + row * DIM + d);
-          sum += from[ROWS * (DIM + 1) + row] * f;
-          acc[0] += v.x * f; acc[1] += v.y * f; acc[2] += v.z * f; acc[3] += v.w * f;
-        }
+    // a warp a row, a lane DIM / 32 of its elements
+    constexpr int E = DIM / 32;
+    for (int row = warp; row < ROWS; row += kAttnWarps) {
+      const bool mine_there = lane < s1 - s0 && list[min(s0 + lane, SLOTS - 1)].tiles > 0;
+      const float* const ref = part_of(min(s0 + lane, SLOTS - 1)) + ROWS * DIM + row;
+      float m = mine_there ? ref[0] : kAttnNoMax, top = m;
+#pragma unroll
+      for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+      top = __shfl_sync(0xffffffffu, top, 0);   // (there are no more than 16 parts: the lower half has the largest)
+      const float f = mine_there ? exp2f(m - top) : 0.f, lf = mine_there ? ref[ROWS] * f : 0.f;
+      float sum = 0.f, acc[E] = {};
+      for (int s = s0; s < s1; s++) {
+        if (list[s].tiles == 0) continue;
+        const float fs = __shfl_sync(0xffffffffu, f, s - s0);
+        sum += __shfl_sync(0xffffffffu, lf, s - s0);
+        const float* const from = part_of(s) + row * DIM + E * lane;
+#pragma unroll
+        for (int k = 0; k < E; k++) acc[k] += from[k] * fs;
+      }
       if (whole) {
         __half* const to = attn_row<DIM>(p, sq, head.seg, ROWS, row);
-        const float f = sum > 0.f ? 1.f / sum : sum;
-        if (to) {
-          const __half2 a = __floats2half2_rn(acc[0] * f, acc[1] * f), b = __floats2half2_rn(acc[2] * f, acc[3] * f);
-          *reinterpret_cast<uint2*>(to + d) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
-        }
+        if (to) attn_store<E>(to + E * lane, acc, sum > 0.f ? 1.f / sum : sum);
       } else {
-        __stcg(reinterpret_cast<float4*>(mine + row * DIM + d), make_float4(acc[0], acc[1], acc[2], acc[3]));
-        if (d == 0) {
+#pragma unroll
+        for (int k = 0; k < E; k += 2) __stcg(reinterpret_cast<float2*>(mine + row * DIM + E * lane + k), make_float2(acc[k], acc[k + 1]));
+        if (lane == 0) {
           __stcg(mine + ROWS * DIM + row, top);
           __stcg(mine + ROWS * (DIM + 1) + row, sum);
         }
@@ -529,24 +571,45 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
       __syncthreads();
       if (*s_joins) {
         __threadfence();
-        for (int x = tid; x < ROWS * DIM / 4; x += kAttnWarps * 32) {
-          const int row = x / (DIM / 4), d = x % (DIM / 4) * 4;
+        for (int row = warp; row < ROWS; row += kAttnWarps) {
           __half* const to = attn_row<DIM>(p, sq, head.seg, ROWS, row);
-          if (!to) continue;
-          float top = kAttnNoMax, sum = 0.f, acc[4] = {};
-#pragma unroll 4
-          for (int c = first; c <= final; c++) top = fmaxf(top, __ldcg(p.parts + ((size_t)c * 2 + (c == first)) * PART + ROWS * DIM + row));
-#pragma unroll 4
-          for (int c = first; c <= final; c++) {
-            const float* const from = p.parts + ((size_t)c * 2 + (c == first)) * PART;
-            const float f = exp2f(__ldcg(from + ROWS * DIM + row) - top);
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(from + row * DIM + d));
-            sum += __ldcg(from + ROWS * (DIM + 1) + row) * f;
-            acc[0] += v.x * f; acc[1] += v.y * f; acc[2] += v.z * f; acc[3] += v.w * f;
+          if (!to) break;   // (the rows behind it are not there either)
+          const int parts = final - first + 1;
+          auto part = [&](int k) { return p.parts + ((size_t)(first + k) * 2 + (k == 0)) * PART; };
+          // references and sums of weights a lane a part, 32 parts at a time; the elements of eight parts are asked for at once
+          float top = kAttnNoMax, sum = 0.f, acc[E] = {};
+          for (int k0 = 0; k0 < parts; k0 += 32) {
+            const bool there = k0 + lane < parts;
+            const float* const ref = part(min(k0 + lane, parts - 1)) + ROWS * DIM + row;
+            const float m = there ? __ldcg(ref) : kAttnNoMax, l = there ? __ldcg(ref + ROWS) : 0.f;
+            float mt = fmaxf(top, m);
+#pragma unroll
+            for (int x = 16; x > 0; x >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, x));
+            const float old = exp2f(top - mt), f = there ? exp2f(m - mt) : 0.f;
+            top = mt;
+            sum *= old;
+#pragma unroll
+            for (int k = 0; k < E; k++) acc[k] *= old;
+            for (int k = 0; k < min(32, parts - k0); k += 8) {
+              float2 v[8][E / 2];
+#pragma unroll
+              for (int u = 0; u < 8; u++)
+#pragma unroll
+                for (int d = 0; d < E / 2; d++)
+                  v[u][d] = k0 + k + u < parts ? __ldcg(reinterpret_cast<const float2*>(part(k0 + k + u) + row * DIM + E * lane) + d) : make_float2(0.f, 0.f);
+#pragma unroll
+              for (int u = 0; u < 8; u++) {
+                const float fu = __shfl_sync(0xffffffffu, f, k + u), lu = __shfl_sync(0xffffffffu, l, k + u);
+                sum += lu * fu;
+#pragma unroll
+                for (int d = 0; d < E / 2; d++) {
+                  acc[2 * d] += v[u][d].x * fu;
+                  acc[2 * d + 1] += v[u][d].y * fu;
+                }
+              }
+            }
           }
-          const float f = sum > 0.f ? 1.f / sum : sum;
-          const __half2 a = __floats2half2_rn(acc[0] * f, acc[1] * f), b = __floats2half2_rn(acc[2] * f, acc[3] * f);
-          *reinterpret_cast<uint2*>(to + d) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+          attn_store<E>(to + E * lane, acc, sum > 0.f ? 1.f / sum : sum);
         }
       }
     }

@@ -1,5 +1,5 @@
 // Attention of many rows of a sequence (prompts, long guesses) over the paged 8-bit cache on tcgen05; the operator is that of
-// kv_attention.cuh, for the sequences whose new tokens times query heads of a key head are more than kAttnFewRows.
+// kv_attention.cuh, for the sequences whose new tokens times query heads of a key head are more than p.few.
 //
 // Bound by the tensor cores and by the exponentials beside them (one for every row and key, 16 a clock and SM).
 // Work. One CTA a key head and 256 rows of a sequence (tokens x query heads that share the key head, token by token), two row tiles of 128.
@@ -19,7 +19,6 @@
 namespace rcp {
 
 constexpr int kPromptThreads = 512, kPromptRows = 256, kPromptKeys = 64, kPromptStages = 4;
-constexpr int kAttnFewRows = 64;   // sequences with no more rows than that go to kv_attention_split_kernel
 
 constexpr uint32_t kPromptPolls = 1u << 18;   // a wait of this kernel is a few microseconds
 
@@ -152,7 +151,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
   // few rows are the other kernel's (which runs beside this one unless there is but one sequence). Behind a wait that gave up nothing
   // more is waited for: the results are invalid already.
   const int gave_up = __syncthreads_or(tid == 0 && *reinterpret_cast<volatile int32_t*>(p.status) != 0);
-  if (gave_up || tile_row < 0 || rows <= 0 || (p.s.seqs > 1 && total_rows <= kAttnFewRows)) {
+  if (gave_up || tile_row < 0 || rows <= 0 || total_rows <= p.few) {
     asm volatile("griddepcontrol.launch_dependents;");
     return;
   }
@@ -164,7 +163,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
   constexpr uint32_t STAGES = kPromptStages;
   const uint32_t k_full = bar, k_empty = k_full + 8 * STAGES, v_full = k_empty + 8 * STAGES, v_empty = v_full + 8 * STAGES;
   const uint32_t s_full = v_empty + 8 * STAGES;                                      // [row tile][buffer]
-  const uint32_t p_full = s_full + 32, o_done = p_full + 16, drained = o_done + 16;   // [row tile]
+  const uint32_t p_full = s_full + 32;                                               // [row tile][buffer]: a warp may be a tile ahead of the others
+  const uint32_t o_done = p_full + 32, drained = o_done + 16;                        // [row tile]
   if (tid == 0) {
     for (uint32_t i = 0; i < STAGES; i++) {
       mbar_init(k_full + 8 * i, 128);
@@ -175,7 +175,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
     for (int i = 0; i < 2; i++) {
       mbar_init(s_full + 16 * i, 1);
       mbar_init(s_full + 16 * i + 8, 1);
-      mbar_init(p_full + 8 * i, 128);
+      mbar_init(p_full + 16 * i, 128);
+      mbar_init(p_full + 16 * i + 8, 128);
       mbar_init(o_done + 8 * i, 1);
       mbar_init(drained + 8 * i, 1);
     }
@@ -294,7 +295,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
         l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        mbar_arrive(p_full + 8 * half);
+        mbar_arrive(p_full + 16 * half + 8 * (t & 1));
       }
       // (one after the other: a wait by parity is good for the phase behind one that is known to be over)
       if (ok && tiles > 1) ok = prompt_wait(o_done + 8 * half, (tiles - 2) & 1);
@@ -443,7 +444,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
           if (!ok) break;
         }
         const int stage = t % kPromptStages;
-        ok = prompt_wait(v_full + 8 * stage, (uint32_t)(t / kPromptStages) & 1u) && prompt_wait(p_full + 8 * half, t & 1);
+        ok = prompt_wait(v_full + 8 * stage, (uint32_t)(t / kPromptStages) & 1u) &&
+             prompt_wait(p_full + 16 * half + 8 * (t & 1), (uint32_t)(t >> 1) & 1u);
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t vb = v0 + (uint32_t)(stage * (L::tile_bytes >> 4));

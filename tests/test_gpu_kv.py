@@ -286,6 +286,24 @@ def test_attention_results_repeat_and_leave_the_workspace_ready():
         assert torch.equal(rcp.rcp_kv_attention(q, cache, *args, workspace=ws), first)
 
 
+@pytest.mark.parametrize("dim,heads,new,length", [(128, 32, 20, 3000), (128, 32, 200, 1500), (64, 16, 40, 5000)])
+def test_attention_of_many_ctas_at_once(dim, heads, new, length):
+    """Enough sequences that every SM is at work and its warps drift apart; several runs, each the same and each right."""
+    page, kv_heads, B = 64, 8, 16
+    lengths = [length - 17 * b for b in range(B)]
+    pages = sum(-(-n // page) for n in lengths)
+    cache = random_cache(pages, kv_heads, page, dim, seed=65)
+    table = make_table(lengths, page, pages, seed=66)
+    args = tensors(starts_of([new] * B), lengths, table)
+    q, ws = rand(B * new, heads, dim, seed=67), rcp.make_kv_workspace(DEV)
+    outs = [rcp.rcp_kv_attention(q, cache, *args, workspace=ws) for _ in range(25)]
+    torch.cuda.synchronize()
+    assert int(ws[:4].view(torch.int32)) == 0
+    want, tol = ref.attention(q, cache, starts_of([new] * B), lengths, table, dim ** -0.5)
+    check_attention(outs[0], want, tol)
+    assert all(torch.equal(o, outs[0]) for o in outs[1:])
+
+
 def test_captured_calls_follow_lengths_and_tables():
     """Append and attention of a decode step captured once; lengths and tables change between replays."""
     page, dim, heads, kv_heads, B = 32, 64, 8, 2, 3
