@@ -169,6 +169,9 @@ int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads,
   p.q = static_cast<const __half*>(q_f16);
   p.q_stride = q_stride;
   p.heads = heads; p.kv_heads = kv_heads; p.group = heads / kv_heads;
+  auto inverse = [](uint32_t d) { return d == 1 ? 0u : (uint32_t)(((uint64_t(1) << 32) + d - 1) / d); };
+  p.group_inv = inverse((uint32_t)p.group);
+  p.kv_heads_inv = inverse((uint32_t)kv_heads);
   p.scale_log2 = sm_scale * 1.4426950408889634f;
   p.k_cache = static_cast<const uint8_t*>(k_cache);
   p.v_cache = static_cast<const uint8_t*>(v_cache);

@@ -32,6 +32,7 @@ struct AttnParams {
   const __half* q;
   long long q_stride;        // elements between tokens
   int heads, kv_heads, group;   // group: query heads of a key head
+  uint32_t group_inv, kv_heads_inv;   // for attn_quotient
   float scale_log2;          // sm_scale * log2(e)
   KvSeqs s;
   const uint8_t *k_cache, *v_cache;
@@ -45,6 +46,7 @@ struct AttnParams {
 
 constexpr int kAttnMaxCtas = 256, kAttnMaxRows = 24;
 constexpr int kAttnWarps = 8, kAttnTile = 32;
+constexpr int kAttnAlone = 4;   // tiles a warp
 constexpr float kAttnSlack = 6.f, kAttnLift = 8.f, kAttnNoMax = -1e30f;
 constexpr size_t kAttnArrivedAt = 256, kAttnPartsAt = kAttnArrivedAt + kAttnMaxCtas * sizeof(int32_t);
 constexpr size_t kAttnWorkspaceBytes = kAttnPartsAt + (size_t)kAttnMaxCtas * 2 * kAttnMaxRows * (128 + 2) * sizeof(float);
@@ -67,6 +69,9 @@ struct AttnLayout {
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
@@ -101,6 +106,9 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return r;
 }
 
+// x / d for x < 2^16 and d <= 1024, with inv = 2^32 / d rounded up (0 for 1): off by less than x / 2^32 < 1 / d before it is cut off
+__device__ __forceinline__ int attn_quotient(int x, uint32_t inv) { return inv ? (int)__umulhi((uint32_t)x, inv) : x; }
+
 // A place in the list of tiles: segment `seg` of sequence b (row tile seg / kv_heads, key head seg % kv_heads), tile of its keys.
 struct AttnPlace {
   int b, seg, tile;
@@ -126,17 +134,18 @@ __device__ __forceinline__ void attn_next_segment(const AttnParams& p, AttnPlace
 
 // what is to be done with a part of a segment in shared memory
 struct alignas(16) AttnPiece {
-  int b, seg, tile0, tiles, of, pad;   // the keys' tiles tile0 .. tile0 + tiles - 1 of `of` (tiles 0: nothing here)
-  long long start;                     // the segment's first tile in the list of all
+  int seg, tile0, tiles, of;   // the keys' tiles tile0 .. tile0 + tiles - 1 of `of` (tiles 0: nothing here)
+  int t0, n;                   // of the sequence
+  long long start;             // the segment's first tile in the list of all: segments differ in it
 };
 
 // y = sums / weights as fp16, to the row's place
 template <int DIM>
-__device__ __forceinline__ __half* attn_row(const AttnParams& p, const KvSeq& sq, int seg, int rows, int row) {
-  const int r = seg / p.kv_heads * rows + row;
-  if (r >= sq.n * p.group) return nullptr;
-  const int i = r / p.group;
-  return p.out + ((long long)(sq.t0 + i) * p.heads + (long long)(seg % p.kv_heads) * p.group + (r - i * p.group)) * DIM;
+__device__ __forceinline__ __half* attn_row(const AttnParams& p, int t0, int n, int seg, int rows, int row) {
+  const int rt = attn_quotient(seg, p.kv_heads_inv), r = rt * rows + row;
+  if (r >= n * p.group) return nullptr;
+  const int i = attn_quotient(r, p.group_inv);
+  return p.out + ((long long)(t0 + i) * p.heads + (long long)(seg - rt * p.kv_heads) * p.group + (r - i * p.group)) * DIM;
 }
 
 template <int E>
@@ -161,17 +170,23 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
 
   // Tiles in front of each sequence, and where this warp's share of them begins. Up to 32 sequences every warp finds that out for itself, a
   // sequence a lane; more are scanned by the CTA.
-  long long total, c0, c1, w0, ctas;
+  long long total, c0, c1, w0, each, more;   // each, more: the first `more` CTAs have each + 1 tiles, the others `each`
+  int ctas;
+  auto quotient = [](long long a, long long b) { return (a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b); };
+  AttnPlace at{};
+  long long in = 0;   // the share's first tile in its sequence
   auto share = [&]() {   // of `total`: as many CTAs as have a tile for each of their warps
-    ctas = min((long long)gridDim.x, (total + kAttnWarps - 1) / kAttnWarps);
-    if ((long long)blockIdx.x >= ctas) return false;
-    c0 = total * blockIdx.x / ctas;
-    c1 = total * (blockIdx.x + 1) / ctas;
+    ctas = (int)min((long long)gridDim.x, (total + kAttnWarps - 1) / kAttnWarps);
+    // (a short sequence on its own: a CTA a segment, whose warps' parts meet in shared memory, is faster than parts that meet in memory)
+    if (p.s.seqs == 1 && at.tiles <= kAttnAlone * kAttnWarps && at.segs <= (int)gridDim.x) ctas = at.segs;
+    if ((int)blockIdx.x >= ctas) return false;
+    each = quotient(total, ctas);
+    more = total - each * ctas;
+    c0 = each * blockIdx.x + min((long long)blockIdx.x, more);
+    c1 = c0 + each + ((int)blockIdx.x < more ? 1 : 0);
     w0 = c0 + (c1 - c0) * warp / kAttnWarps;
     return true;
   };
-  AttnPlace at{};
-  long long in = 0;   // the share's first tile in its sequence
   if (p.s.seqs <= 32) {
     if (lane < p.s.seqs) attn_sequence<ROWS>(p, lane, at);
     const long long mine = (long long)at.segs * at.tiles;
@@ -182,6 +197,10 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
       if (lane >= d) upto += o;
     }
     total = __shfl_sync(0xffffffffu, upto, 31);
+    if (p.s.seqs == 1) {   // (what follows, without the votes)
+      at.segs = __shfl_sync(0xffffffffu, at.segs, 0);
+      at.tiles = __shfl_sync(0xffffffffu, at.tiles, 0);
+    }
     if (!share()) return;
     // the last sequence with no more than w0 tiles in front of it (it has some itself, or there is nothing to do)
     const int b = 31 - __clz((int)__ballot_sync(0xffffffffu, lane < p.s.seqs && upto - mine <= w0));
@@ -240,7 +259,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
   }
   const int todo = (int)min(c0 + (c1 - c0) * (warp + 1) / kAttnWarps - w0, (long long)INT_MAX);
   if (todo > 0) {
-    at.seg = (int)(in / at.tiles);
+    at.seg = (int)quotient(in, at.tiles);
     at.tile = (int)(in - (long long)at.seg * at.tiles);
   }
   if (lane < 2) list[2 * warp + lane].tiles = 0;   // (written again and read by this warp, then by all behind a barrier)
@@ -251,6 +270,11 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
     float* const metaf = reinterpret_cast<float*>(attn_shared + L::meta) + warp * S * 4;
     AttnPlace ld = at;
     int loaded = 0, ld_stage = 0, pages_at = -1, pages_b = -1, my_page = -1;
+    // where a lane's 16-byte pieces go, every 512 bytes one: piece c of a row, exchanged within 128 bytes so that the reads below meet no bank twice
+    const int row0 = lane / (DIM / 16), line0 = DIM == 128 ? row0 : row0 >> 1, in0 = DIM == 128 ? lane & 7 : (row0 & 1) * 4 + (lane & 3);
+    const uint32_t k_to = (uint32_t)(line0 * 128 + ((DIM == 128 ? in0 ^ ((row0 & 1) << 2) : in0) << 4));
+    const uint32_t v_to0 = (uint32_t)(L::tile_bytes + line0 * 128 + ((in0 ^ (((row0 >> 1) & 3) << 1)) << 4));
+    const uint32_t v_to1 = DIM == 128 ? v_to0 ^ 64u : v_to0;   // (rows four further on)
     // asks for the next tile
     auto load = [&]() {
       if (loaded < todo) {
@@ -263,20 +287,25 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
         }
         const int pg = __shfl_sync(0xffffffffu, my_page, ld.tile - pages_at), j0 = ld.tile * kAttnTile;
         const bool there = pg >= 0 && pg < p.s.pages;
-        const int kv = ld.seg % p.kv_heads;
+        const int kv = ld.seg - attn_quotient(ld.seg, p.kv_heads_inv) * p.kv_heads;
         const long long block = there ? (long long)pg * p.kv_heads + kv : 0;
-        const long long off = (block * p.s.page + (j0 & (p.s.page - 1))) * DIM;
+        const long long off = (block * p.s.page + (j0 & (p.s.page - 1))) * DIM + lane * 16;
         const int live = there ? min(ld.sq.end - j0, kAttnTile) : 0;   // keys of the tile that exist: the others are zeroes
         const uint32_t dst = ring + (uint32_t)(ld_stage * L::stage_bytes);
+        const uint8_t *const k_from = p.k_cache + off, *const v_from = p.v_cache + off;
+        if (live == kAttnTile) {
 #pragma unroll
-        for (int i = 0; i < DIM / 16; i++) {
-          const int n = lane + 32 * i, row = n / (DIM / 16), c = n % (DIM / 16);
-          const int line = DIM == 128 ? row : row >> 1, in = DIM == 128 ? c : (row & 1) * 4 + c;
-          const int kc = DIM == 128 ? in ^ ((row & 1) << 2) : in, vc = in ^ (((row >> 1) & 3) << 1);
-          const int bytes = row < live ? 16 : 0;
-          const long long from = off + (long long)(bytes ? row * DIM + c * 16 : 0);
-          cp_async16(dst + line * 128 + kc * 16, p.k_cache + from, bytes);
-          cp_async16(dst + L::tile_bytes + line * 128 + vc * 16, p.v_cache + from, bytes);
+          for (int i = 0; i < DIM / 16; i++) {
+            cp_async16(dst + k_to + i * 512, k_from + i * 512);
+            cp_async16(dst + (i & 1 ? v_to1 : v_to0) + i * 512, v_from + i * 512);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < DIM / 16; i++) {
+            const int bytes = (lane + 32 * i) / (DIM / 16) < live ? 16 : 0;   // (nothing is read where it is zero)
+            cp_async16(dst + k_to + i * 512, bytes ? k_from + i * 512 : p.k_cache, bytes);
+            cp_async16(dst + (i & 1 ? v_to1 : v_to0) + i * 512, bytes ? v_from + i * 512 : p.v_cache, bytes);
+          }
         }
         float* const m = metaf + ld_stage * 4;
         if (lane == 0) cp_async4(attn_smem(m), p.k_scale + block);
@@ -296,10 +325,10 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
     int lim[NT][2], least = 0;
     // queries and limits of a segment; sums at zero
     auto begin = [&]() {
-      const int kv = at.seg % p.kv_heads, r0 = at.seg / p.kv_heads * ROWS, rows = at.sq.n * p.group;
+      const int rt = attn_quotient(at.seg, p.kv_heads_inv), kv = at.seg - rt * p.kv_heads, r0 = rt * ROWS, rows = at.sq.n * p.group;
 #pragma unroll
       for (int n = 0; n < NT; n++) {
-        const int r = r0 + n * 8 + g, i = r / p.group;
+        const int r = r0 + n * 8 + g, i = attn_quotient(r, p.group_inv);
         const bool have = r < rows;
         const __half* const src = p.q + (have ? (long long)(at.sq.t0 + i) * p.q_stride + (long long)(kv * p.group + r - i * p.group) * DIM : 0);
 #pragma unroll
@@ -312,7 +341,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
         least = n == 0 ? INT_MAX : least;
 #pragma unroll
         for (int e = 0; e < 2; e++) {
-          const int rr = r0 + n * 8 + 2 * j + e, pos = at.sq.first + rr / p.group;
+          const int rr = r0 + n * 8 + 2 * j + e, pos = at.sq.first + attn_quotient(rr, p.group_inv);
           lim[n][e] = rr >= rows ? INT_MAX : pos >= 0 && pos < at.sq.end ? pos + 1 : 0;
           least = min(least, lim[n][e]);
           m[n][e] = kAttnNoMax;
@@ -334,7 +363,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
         for (int n = 0; n < NT; n++)
 #pragma unroll
           for (int e = 0; e < 2; e++) {
-            __half* const to = attn_row<DIM>(p, at.sq, at.seg, ROWS, n * 8 + 2 * j + e);
+            __half* const to = attn_row<DIM>(p, at.sq.t0, at.sq.n, at.seg, ROWS, n * 8 + 2 * j + e);
             const float f = l[n][e] > 0.f ? vs / l[n][e] : l[n][e];   // no keys: zero (and a sum that is no number stays one)
             if (to) {
 #pragma unroll
@@ -366,7 +395,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
             part[ROWS * (DIM + 1) + row] = l[n][e];
           }
         }
-      if (lane == 0) list[2 * warp + (last ? 1 : 0)] = AttnPiece{at.b, at.seg, t0, t1 - t0, at.tiles, 0, unit + 1 - t1};
+      if (lane == 0) list[2 * warp + (last ? 1 : 0)] = AttnPiece{at.seg, t0, t1 - t0, at.tiles, at.sq.t0, at.sq.n, unit + 1 - t1};
     };
 
     begin();
@@ -376,7 +405,8 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
       __syncwarp();
       load();
       const uint32_t kt = ring + (uint32_t)(stage * L::stage_bytes), vt = kt + L::tile_bytes;
-      const float ks = metaf[stage * 4], vs_new = metaf[stage * 4 + 1], there = metaf[stage * 4 + 2];
+      const float4 meta = *reinterpret_cast<const float4*>(metaf + stage * 4);
+      const float ks = meta.x, vs_new = meta.y, there = meta.z;
       if (++stage == S) stage = 0;
       float s[2][NT][4];
 #pragma unroll
@@ -513,42 +543,45 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
   auto part_of = [&](int slot) {
     return reinterpret_cast<const float*>(attn_shared + ((slot & 1) ? (slot >> 1) * S * L::stage_bytes : L::first + (slot >> 1) * PART * 4));
   };
-  for (int s0 = 0; s0 < SLOTS;) {
-    if (list[s0].tiles == 0) { s0++; continue; }
-    const AttnPiece head = list[s0];
-    int s1 = s0, tiles = 0;
-    for (; s1 < SLOTS; s1++) {
-      const AttnPiece e = list[s1];
-      if (e.tiles == 0) continue;
-      if (e.b != head.b || e.seg != head.seg) break;
-      tiles += e.tiles;
-    }
-    const KvSeq sq = kv_seq(p.s, head.b);
-    const bool whole = tiles == head.of;
-    const int slot = head.tile0 > 0 ? 0 : 1;   // of a segment that does not begin here the first slot, of one that does not end here the second
-    float* const mine = p.parts + ((size_t)blockIdx.x * 2 + slot) * PART;
-    // a warp a row, a lane DIM / 32 of its elements
-    constexpr int E = DIM / 32;
+  // A piece a lane; the first lane of each run of pieces of a segment stands for the run. A warp takes a row, a lane DIM / 32 of its elements.
+  constexpr int E = DIM / 32;
+  const AttnPiece piece = list[lane % SLOTS];
+  const uint32_t valid = __ballot_sync(0xffffffffu, lane < SLOTS && piece.tiles > 0);
+  const uint32_t in_front = valid & ((1u << lane) - 1);
+  const long long start_in_front = __shfl_sync(0xffffffffu, piece.start, in_front ? 31 - __clz((int)in_front) : 0);
+  const uint32_t heads = __ballot_sync(0xffffffffu, (valid >> lane & 1) && (!in_front || start_in_front != piece.start));
+  uint32_t open = 0;   // runs that are not the whole of their segment: two at most, the first and the last
+  for (uint32_t todo_runs = heads; todo_runs; todo_runs &= todo_runs - 1) {
+    const int s0 = __ffs((int)todo_runs) - 1;
+    const uint32_t behind = heads & ~((2u << s0) - 1), members = valid & (behind ? (1u << (__ffs((int)behind) - 1)) - 1 : ~0u) & ~((1u << s0) - 1);
+    const bool member = members >> lane & 1;
+    const int tiles = __reduce_add_sync(0xffffffffu, member ? piece.tiles : 0);
+    const int seg = __shfl_sync(0xffffffffu, piece.seg, s0), t0 = __shfl_sync(0xffffffffu, piece.t0, s0), n = __shfl_sync(0xffffffffu, piece.n, s0);
+    const bool whole = tiles == __shfl_sync(0xffffffffu, piece.of, s0);
+    // of a segment that does not begin here the first slot, of one that does not end here the second
+    float* const mine = p.parts + ((size_t)blockIdx.x * 2 + (__shfl_sync(0xffffffffu, piece.tile0, s0) > 0 ? 0 : 1)) * PART;
+    if (!whole) open |= 1u << s0;
     for (int row = warp; row < ROWS; row += kAttnWarps) {
-      const bool mine_there = lane < s1 - s0 && list[min(s0 + lane, SLOTS - 1)].tiles > 0;
-      const float* const ref = part_of(min(s0 + lane, SLOTS - 1)) + ROWS * DIM + row;
-      float m = mine_there ? ref[0] : kAttnNoMax, top = m;
+      __half* const to = attn_row<DIM>(p, t0, n, seg, ROWS, row);
+      if (!to) break;   // (the rows behind it are not there either)
+      const float* const ref = part_of(lane % SLOTS) + ROWS * DIM + row;
+      const float m = member ? ref[0] : kAttnNoMax;
+      float top = m;
 #pragma unroll
-      for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-      top = __shfl_sync(0xffffffffu, top, 0);   // (there are no more than 16 parts: the lower half has the largest)
-      const float f = mine_there ? exp2f(m - top) : 0.f, lf = mine_there ? ref[ROWS] * f : 0.f;
+      for (int x = SLOTS / 2; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x, SLOTS));
+      top = __shfl_sync(0xffffffffu, top, 0);
+      const float f = member ? exp2f(m - top) : 0.f, lf = member ? ref[ROWS] * f : 0.f;
       float sum = 0.f, acc[E] = {};
-      for (int s = s0; s < s1; s++) {
-        if (list[s].tiles == 0) continue;
-        const float fs = __shfl_sync(0xffffffffu, f, s - s0);
-        sum += __shfl_sync(0xffffffffu, lf, s - s0);
+      for (uint32_t left = members; left; left &= left - 1) {
+        const int s = __ffs((int)left) - 1;
+        const float fs = __shfl_sync(0xffffffffu, f, s);
+        sum += __shfl_sync(0xffffffffu, lf, s);
         const float* const from = part_of(s) + row * DIM + E * lane;
 #pragma unroll
         for (int k = 0; k < E; k++) acc[k] += from[k] * fs;
       }
       if (whole) {
-        __half* const to = attn_row<DIM>(p, sq, head.seg, ROWS, row);
-        if (to) attn_store<E>(to + E * lane, acc, sum > 0.f ? 1.f / sum : sum);
+        attn_store<E>(to + E * lane, acc, sum > 0.f ? 1.f / sum : sum);
       } else {
 #pragma unroll
         for (int k = 0; k < E; k += 2) __stcg(reinterpret_cast<float2*>(mine + row * DIM + E * lane + k), make_float2(acc[k], acc[k + 1]));
@@ -558,62 +591,71 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
         }
       }
     }
-    if (!whole) {
-      // the last of the CTAs that have parts of this segment to arrive here joins them
-      const int first = (int)(((head.start + 1) * ctas - 1) / total), final = (int)(((head.start + head.of) * ctas - 1) / total);
-      __threadfence();
-      __syncthreads();
-      if (tid == 0) {
-        const int n = atomicAdd(p.arrived + first, 1);
-        if (n == final - first) p.arrived[first] = 0;
-        *s_joins = n == final - first;
-      }
-      __syncthreads();
-      if (*s_joins) {
-        __threadfence();
-        for (int row = warp; row < ROWS; row += kAttnWarps) {
-          __half* const to = attn_row<DIM>(p, sq, head.seg, ROWS, row);
-          if (!to) break;   // (the rows behind it are not there either)
-          const int parts = final - first + 1;
-          auto part = [&](int k) { return p.parts + ((size_t)(first + k) * 2 + (k == 0)) * PART; };
-          // references and sums of weights a lane a part, 32 parts at a time; the elements of eight parts are asked for at once
-          float top = kAttnNoMax, sum = 0.f, acc[E] = {};
-          for (int k0 = 0; k0 < parts; k0 += 32) {
-            const bool there = k0 + lane < parts;
-            const float* const ref = part(min(k0 + lane, parts - 1)) + ROWS * DIM + row;
-            const float m = there ? __ldcg(ref) : kAttnNoMax, l = there ? __ldcg(ref + ROWS) : 0.f;
-            float mt = fmaxf(top, m);
+  }
+  if (!open) return;
+  // The last of the CTAs that have parts of a segment to arrive here joins them.
+  auto owner = [&](long long unit) {
+    const long long big = more * (each + 1);
+    return (int)(unit < big ? quotient(unit, each + 1) : more + quotient(unit - big, each));
+  };
+  int first = 0, final = 0;   // CTAs with parts of the lane's segment
+  if (open >> lane & 1) {
+    first = owner(piece.start);
+    final = owner(piece.start + piece.of - 1);
+  }
+  __threadfence();
+  __syncthreads();
+  if (warp == 0 && (open >> lane & 1)) {
+    const int n = atomicAdd(p.arrived + first, 1);
+    if (n == final - first) p.arrived[first] = 0;
+    s_joins[open & ((1u << lane) - 1) ? 1 : 0] = n == final - first;
+  }
+  __syncthreads();
+  for (int k = 0; open; k++, open &= open - 1) {
+    if (!s_joins[k]) continue;
+    __threadfence();
+    const int s0 = __ffs((int)open) - 1;
+    const int cta0 = __shfl_sync(0xffffffffu, first, s0), parts = __shfl_sync(0xffffffffu, final, s0) - cta0 + 1;
+    const int seg = __shfl_sync(0xffffffffu, piece.seg, s0), t0 = __shfl_sync(0xffffffffu, piece.t0, s0), n = __shfl_sync(0xffffffffu, piece.n, s0);
+    auto part = [&](int k) { return p.parts + ((size_t)(cta0 + k) * 2 + (k == 0)) * PART; };
+    for (int row = warp; row < ROWS; row += kAttnWarps) {
+      __half* const to = attn_row<DIM>(p, t0, n, seg, ROWS, row);
+      if (!to) break;
+      // references and sums of weights a lane a part, 32 parts at a time; the elements of eight parts are asked for at once
+      float top = kAttnNoMax, sum = 0.f, acc[E] = {};
+      for (int k0 = 0; k0 < parts; k0 += 32) {
+        const bool there = k0 + lane < parts;
+        const float* const ref = part(min(k0 + lane, parts - 1)) + ROWS * DIM + row;
+        const float m = there ? __ldcg(ref) : kAttnNoMax, l = there ? __ldcg(ref + ROWS) : 0.f;
+        float mt = fmaxf(top, m);
 #pragma unroll
-            for (int x = 16; x > 0; x >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, x));
-            const float old = exp2f(top - mt), f = there ? exp2f(m - mt) : 0.f;
-            top = mt;
-            sum *= old;
+        for (int x = 16; x > 0; x >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, x));
+        const float old = exp2f(top - mt), f = there ? exp2f(m - mt) : 0.f;
+        top = mt;
+        sum *= old;
 #pragma unroll
-            for (int k = 0; k < E; k++) acc[k] *= old;
-            for (int k = 0; k < min(32, parts - k0); k += 8) {
-              float2 v[8][E / 2];
+        for (int k = 0; k < E; k++) acc[k] *= old;
+        for (int k = 0; k < min(32, parts - k0); k += 8) {
+          float2 v[8][E / 2];
 #pragma unroll
-              for (int u = 0; u < 8; u++)
+          for (int u = 0; u < 8; u++)
 #pragma unroll
-                for (int d = 0; d < E / 2; d++)
-                  v[u][d] = k0 + k + u < parts ? __ldcg(reinterpret_cast<const float2*>(part(k0 + k + u) + row * DIM + E * lane) + d) : make_float2(0.f, 0.f);
+            for (int d = 0; d < E / 2; d++)
+              v[u][d] = k0 + k + u < parts ? __ldcg(reinterpret_cast<const float2*>(part(k0 + k + u) + row * DIM + E * lane) + d) : make_float2(0.f, 0.f);
 #pragma unroll
-              for (int u = 0; u < 8; u++) {
-                const float fu = __shfl_sync(0xffffffffu, f, k + u), lu = __shfl_sync(0xffffffffu, l, k + u);
-                sum += lu * fu;
+          for (int u = 0; u < 8; u++) {
+            const float fu = __shfl_sync(0xffffffffu, f, k + u), lu = __shfl_sync(0xffffffffu, l, k + u);
+            sum += lu * fu;
 #pragma unroll
-                for (int d = 0; d < E / 2; d++) {
-                  acc[2 * d] += v[u][d].x * fu;
-                  acc[2 * d + 1] += v[u][d].y * fu;
-                }
-              }
+            for (int d = 0; d < E / 2; d++) {
+              acc[2 * d] += v[u][d].x * fu;
+              acc[2 * d + 1] += v[u][d].y * fu;
             }
           }
-          attn_store<E>(to + E * lane, acc, sum > 0.f ? 1.f / sum : sum);
         }
       }
+      attn_store<E>(to + E * lane, acc, sum > 0.f ? 1.f / sum : sum);
     }
-    s0 = s1;
   }
 }
 
