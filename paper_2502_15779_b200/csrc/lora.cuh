@@ -65,7 +65,7 @@ struct LoraFewShared {
 // the cluster's tokens (count of them, the same adapter i): G is how many the registers are for
 template <int G>
 __device__ __forceinline__ void lora_few(const LoraParams& p, LoraFewShared& s, int i, int count, uint32_t cta) {
-  constexpr int RB = G == 1 ? 4 : 2;   // rows of a at a time
+  constexpr int RB = G <= 2 ? 4 : 2;   // rows of a at a time
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, R = p.rank;
   const int units = p.K / 8, u0 = (int)((long long)units * cta / kLoraCluster), u1 = (int)((long long)units * (cta + 1) / kLoraCluster);
   const uint4* const a = reinterpret_cast<const uint4*>(p.a + (long long)i * R * p.K);
@@ -77,7 +77,7 @@ __device__ __forceinline__ void lora_few(const LoraParams& p, LoraFewShared& s, 
     const uint4* row[RB];
 #pragma unroll
     for (int r = 0; r < RB; r++) row[r] = a + (long long)min(r0 + r, R - 1) * units;
-#pragma unroll(G == 1 ? 4 : 1)
+#pragma unroll(G == 1 ? 4 : G == 2 ? 2 : 1)
     for (int u = u0 + lane; u < u1; u += 32) {
       float av[RB][8];
 #pragma unroll
@@ -102,46 +102,81 @@ __device__ __forceinline__ void lora_few(const LoraParams& p, LoraFewShared& s, 
         if (r0 + r < R && t < count && lane < kLoraCluster) st_cluster(&s.part[cta][t][r0 + r], lane, v);
       }
   }
-  // rows of b on their way (at most 32 columns of the first rows), and what they are added to
+  // Rows of b a few at a time, sixteen bytes of each asked for together with what they are added to (one row at a time, each waited for, took
+  // half of the call); the first of them in front of the barrier.
   const int n0 = (int)((long long)p.N * cta / kLoraCluster), n1 = (int)((long long)p.N * (cta + 1) / kLoraCluster), V = R / 8;
   const uint4* const b = reinterpret_cast<const uint4*>(p.b + (long long)i * p.N * R);
-  constexpr int PF = 4;
-  uint4 pre[PF];
+  constexpr int ROWS = G == 1 ? 4 : 2, VB = 2;   // rows at a time, 16-byte pieces of each at a time
+  uint4 bv[ROWS][VB];
+  __half base[ROWS][G];
+  auto ask_b = [&](int n, int v0) {
 #pragma unroll
-  for (int v = 0; v < PF; v++)
-    if (n0 + tid < n1 && v < V) pre[v] = __ldg(b + (long long)(n0 + tid) * V + v);
+    for (int r = 0; r < ROWS; r++)
+#pragma unroll
+      for (int v = 0; v < VB; v++)
+        bv[r][v] = n + r * kLoraThreads < n1 && v0 + v < V ? __ldg(b + (long long)(n + r * kLoraThreads) * V + v0 + v) : make_uint4(0, 0, 0, 0);
+  };
+  auto ask_base = [&](int n) {
+#pragma unroll
+    for (int r = 0; r < ROWS; r++)
+#pragma unroll
+      for (int t = 0; t < G; t++)
+        base[r][t] = p.base && t < count && n + r * kLoraThreads < n1 ? p.base[(long long)s.token[t] * p.N + n + r * kLoraThreads] : __float2half_rn(0.f);
+  };
+  int n = n0 + tid;
+  ask_b(n, 0);
+  ask_base(n);
   cluster_barrier();
   const float scale = p.scaling[i];
-  for (int e = tid; e < count * R; e += kLoraThreads) {
-    const int t = e / R, r = e - t * R;
+  for (int e = tid; e < kLoraGroup * kLoraMaxRank; e += kLoraThreads) {
+    const int t = e / kLoraMaxRank, r = e % kLoraMaxRank;
+    if (t >= count || r >= R) continue;
     float sum = 0.f;
 #pragma unroll
     for (int c = 0; c < kLoraCluster; c++) sum += s.part[c][t][r];
     s.z[t][r] = sum * scale;
   }
   __syncthreads();
-  for (int n = n0 + tid; n < n1; n += kLoraThreads) {
-    float y[G] = {};
-    const uint4* const row = b + (long long)n * V;
-#pragma unroll 4
-    for (int v = 0; v < V; v++) {
-      float bv[8];
-      if (n == n0 + tid && v < PF) halves8(v == 0 ? pre[0] : v == 1 ? pre[1] : v == 2 ? pre[2] : pre[3], bv);
-      else halves8(__ldg(row + v), bv);
+  for (; n < n1; n += ROWS * kLoraThreads) {
+    float y[ROWS][G] = {};
+    for (int v0 = 0; v0 < V; v0 += VB) {
+      float w[ROWS][VB][8];
 #pragma unroll
-      for (int t = 0; t < G; t++)
-        if (t < count) {
-          const float4 z0 = *reinterpret_cast<const float4*>(&s.z[t][8 * v]), z1 = *reinterpret_cast<const float4*>(&s.z[t][8 * v + 4]);
-          y[t] = fmaf(bv[0], z0.x, y[t]); y[t] = fmaf(bv[1], z0.y, y[t]); y[t] = fmaf(bv[2], z0.z, y[t]); y[t] = fmaf(bv[3], z0.w, y[t]);
-          y[t] = fmaf(bv[4], z1.x, y[t]); y[t] = fmaf(bv[5], z1.y, y[t]); y[t] = fmaf(bv[6], z1.z, y[t]); y[t] = fmaf(bv[7], z1.w, y[t]);
-        }
+      for (int r = 0; r < ROWS; r++)
+#pragma unroll
+        for (int v = 0; v < VB; v++) halves8(bv[r][v], w[r][v]);
+      if (v0 + VB < V) ask_b(n, v0 + VB);
+#pragma unroll
+      for (int v = 0; v < VB; v++) {
+        if (v0 + v >= V) break;
+#pragma unroll
+        for (int t = 0; t < G; t++)
+          if (t < count) {
+            const float4 z0 = *reinterpret_cast<const float4*>(&s.z[t][8 * (v0 + v)]), z1 = *reinterpret_cast<const float4*>(&s.z[t][8 * (v0 + v) + 4]);
+            const float z[8] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w};
+#pragma unroll
+            for (int r = 0; r < ROWS; r++)
+#pragma unroll
+              for (int k = 0; k < 8; k++) y[r][t] = fmaf(w[r][v][k], z[k], y[r][t]);
+          }
+      }
+    }
+    __half out[ROWS][G];
+#pragma unroll
+    for (int r = 0; r < ROWS; r++)
+#pragma unroll
+      for (int t = 0; t < G; t++) out[r][t] = __float2half_rn(__half2float(base[r][t]) + y[r][t]);
+    // the next rows before these are stored
+    const int now = n;
+    if (n + ROWS * kLoraThreads < n1) {
+      ask_b(n + ROWS * kLoraThreads, 0);
+      ask_base(n + ROWS * kLoraThreads);
     }
 #pragma unroll
-    for (int t = 0; t < G; t++)
-      if (t < count) {
-        const long long at = (long long)s.token[t] * p.N + n;
-        p.y[at] = __float2half_rn(p.base ? __half2float(p.base[at]) + y[t] : y[t]);
-      }
+    for (int r = 0; r < ROWS; r++)
+#pragma unroll
+      for (int t = 0; t < G; t++)
+        if (t < count && now + r * kLoraThreads < n1) p.y[(long long)s.token[t] * p.N + now + r * kLoraThreads] = out[r][t];
   }
 }
 
@@ -177,6 +212,8 @@ __global__ void __cluster_dims__(kLoraCluster, 1, 1) __launch_bounds__(kLoraThre
   // every CTA of the cluster runs before its shared memory is written to from the others
   cluster_barrier();
   if (count == 1) lora_few<1>(p, s, i, count, cta);
+  else if (count == 2) lora_few<2>(p, s, i, count, cta);
+  else if (count <= 4) lora_few<4>(p, s, i, count, cta);
   else lora_few<kLoraGroup>(p, s, i, count, cta);
 }
 
