@@ -87,6 +87,25 @@ int attn_prompt(const rcp::AttnParams& p, cudaStream_t st) {
   return RCP_OK;
 }
 
+template <int STEPS>
+int lora_up(rcp::LoraParams p, int tiles, cudaStream_t st) {
+  using L = rcp::UpLayout<STEPS>;
+  static std::mutex mu;
+  static bool done[kMaxDevices] = {};
+  RCP_CUDA(set_max_smem(rcp::lora_up_kernel<STEPS>, L::bytes, mu, done));
+  // Column tiles of a CTA: few waves of CTAs, and short ones, because tiles in which tokens of two requests meet take twice as long (2011 tokens of
+  // six requests, 28672 columns: 8 tiles a CTA, whose fourth wave is all but empty, 105 us a call; one wave of 25 tiles 146; 5 tiles RESULT).
+  const int cols = (p.N + rcp::kUpCols - 1) / rcp::kUpCols, at_once = sm_count() * std::min<int>(3, 232448 / (L::bytes + 2048));
+  double least = 0;
+  for (int n = 1; n <= std::min(cols, 16); n++) {
+    const int64_t ctas = (int64_t)((cols + n - 1) / n) * tiles;
+    const double cost = (double)((ctas + at_once - 1) / at_once + 1) * (n + 1.5);   // (a CTA's beginning is one tile and a half)
+    if (n == 1 || cost < least) { least = cost; p.up_tiles = n; }
+  }
+  RCP_CUDA(launch_overlapped(rcp::lora_up_kernel<STEPS>, dim3((cols + p.up_tiles - 1) / p.up_tiles, tiles), dim3(rcp::kLoraThreads), L::bytes, st, p));
+  return RCP_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -211,7 +230,7 @@ int rcp_lora_add(const void* x_f16, int64_t x_stride, const void* a_f16, const v
     return RCP_ERR_ALIGN;
   rcp::LoraParams p{static_cast<const __half*>(x_f16), x_stride, static_cast<const __half*>(a_f16), static_cast<const __half*>(b_f16), adapter,
                     scaling, static_cast<const __half*>(base_f16), static_cast<__half*>(y_f16), static_cast<float*>(workspace), M, N, K, rank, adapters,
-                    1, N % 8 == 0 && aligned16(base_f16) && aligned16(y_f16)};
+                    1, N % 8 == 0 && aligned16(base_f16) && aligned16(y_f16), 1};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (M <= rcp::kLoraFew) {
     RCP_CUDA(launch_overlapped(rcp::lora_few_kernel, dim3(M * rcp::kLoraCluster), dim3(rcp::kLoraThreads), 0, st, p));
@@ -225,11 +244,16 @@ int rcp_lora_add(const void* x_f16, int64_t x_stride, const void* a_f16, const v
   static bool done[kMaxDevices] = {};
   RCP_CUDA(set_max_smem(rcp::lora_down_kernel, (int)rcp::lora_down_smem(rcp::kLoraMaxRank), mu, done));
   RCP_CUDA(launch_clustered(rcp::lora_down_kernel, dim3(tiles * p.parts), dim3(rcp::kLoraThreads), rcp::lora_down_smem(rank), p.parts, st, p));
-  constexpr int cols = rcp::kUpCols * rcp::kUpTiles;
-  static constexpr decltype(&rcp::lora_up_kernel<1>) up[8] = {rcp::lora_up_kernel<1>, rcp::lora_up_kernel<2>, rcp::lora_up_kernel<3>, rcp::lora_up_kernel<4>,
-                                                              rcp::lora_up_kernel<5>, rcp::lora_up_kernel<6>, rcp::lora_up_kernel<7>, rcp::lora_up_kernel<8>};
-  RCP_CUDA(launch_overlapped(up[(rank - 1) / 16], dim3((N + cols - 1) / cols, tiles), dim3(rcp::kLoraThreads), 0, st, p));
-  return RCP_OK;
+  switch ((rank - 1) / 16) {
+    case 0: return lora_up<1>(p, tiles, st);
+    case 1: return lora_up<2>(p, tiles, st);
+    case 2: return lora_up<3>(p, tiles, st);
+    case 3: return lora_up<4>(p, tiles, st);
+    case 4: return lora_up<5>(p, tiles, st);
+    case 5: return lora_up<6>(p, tiles, st);
+    case 6: return lora_up<7>(p, tiles, st);
+    default: return lora_up<8>(p, tiles, st);
+  }
 }
 
 }  // extern "C"

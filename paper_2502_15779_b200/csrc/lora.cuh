@@ -27,6 +27,7 @@ struct LoraParams {
   int M, N, K, rank, adapters;
   int parts;                 // CTAs of a cluster of lora_down_kernel: parts of K
   int wide;                  // rows of base and y start on 16 bytes
+  int up_tiles;              // column tiles of a CTA of lora_up_kernel
 };
 
 constexpr int kLoraThreads = 256, kLoraWarps = kLoraThreads / 32;
@@ -222,6 +223,12 @@ __device__ __forceinline__ void lora_mma(float (&c)[4], uint32_t a0, uint32_t a1
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+// the same with sums of zero in front
+__device__ __forceinline__ void lora_mma_first(float (&c)[4], uint4 a, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1), "f"(0.f));
+}
+
 constexpr int kLoraTile = 64;   // tokens of a tile
 struct LoraTokens {
   int adapter[kLoraTile];   // of the tile's tokens, -1: none
@@ -371,27 +378,89 @@ __global__ void __launch_bounds__(kLoraThreads) lora_down_kernel(const LoraParam
   }
 }
 
-constexpr int kUpCols = 128, kUpTiles = 8;   // columns of a tile (32 a warp), tiles of a CTA
-struct LoraUpShared {
-  __half z[2][kLoraTile][kLoraMaxRank + 16];   // upper and lower part of z / 2^exponent
-  float unit[kLoraTile];
-  LoraTokens t;
+constexpr int kUpCols = 128;   // columns of a tile (32 a warp); a CTA has p.up_tiles of them, so many that all CTAs run at once
+// shared memory of lora_up_kernel: z, two stages of a tile's rows of b, three of what is added to; rows with gaps against bank conflicts
+template <int STEPS>
+struct UpLayout {
+  static constexpr int row = STEPS * 16 + 16;                       // halves of a row of b
+  // z as the tensor core wants it: [upper, lower parts][16 tokens][step] of 512 bytes, a lane's 16 bytes of each side by side
+  static constexpr int z = 0, stage0 = 2 * (kLoraTile / 16) * STEPS * 512;
+  static constexpr int b_bytes = kUpCols * row * 2, base_row = kUpCols * 2 + 16, add_bytes = kLoraTile * base_row;
+  static constexpr int add0 = stage0 + 2 * b_bytes, bytes = add0 + 3 * add_bytes;   // (what comes from far away is asked for one tile earlier)
 };
-// y of kLoraTile tokens x kUpTiles * kUpCols columns; a warp has half of the tile's tokens and 32 columns, and asks for what it adds to first. Column c of n-tile n is column
+// y of kLoraTile tokens x p.up_tiles * kUpCols columns; a warp has half of the tile's tokens and 32 columns. Column c of n-tile n is column
 // 8 (c / 2) + 2 n + c % 2 of the 32, so that a thread's sums of a row are eight columns side by side and meet base and y in 16 bytes.
+// The next tile's rows of b and of base are on their way to shared memory meanwhile (fragments and base straight from memory: 98 us at 2011
+// tokens, 28672 columns, rank 64, bound by the latency of what was in flight).
 // STEPS: the rank in steps of 16, rounded up
 template <int STEPS>
-__global__ void __launch_bounds__(kLoraThreads, 2) lora_up_kernel(const LoraParams p) {
-  __shared__ __align__(16) LoraUpShared s;
+__global__ void __launch_bounds__(kLoraThreads, STEPS <= 4 ? 2 : 1) lora_up_kernel(const LoraParams p) {
+  using L = UpLayout<STEPS>;
+  extern __shared__ __align__(128) uint8_t lora_shared[];
+  __shared__ LoraTokens s;
+  __shared__ float s_unit[kLoraTile];
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, j = lane & 3, R = p.rank;
+  const uint32_t base = (uint32_t)__cvta_generic_to_shared(lora_shared);
   const int m0 = (int)blockIdx.y * kLoraTile;
-  const int different = tile_adapters(p, m0, s.t);
+  const int different = tile_adapters(p, m0, s);
+  // passes of a tile: the adapters, and the rows without any if there are some
+  const bool none = __syncthreads_or(tid < kLoraTile && m0 + tid < p.M && s.adapter[tid] < 0);
+  const int passes = different + (none ? 1 : 0), first = (int)blockIdx.x * p.up_tiles, tiles = min(p.up_tiles, (p.N + kUpCols - 1) / kUpCols - first);
+  // Copies of a thread, 16 bytes each: of b every second piece of one row, of base a piece of every sixteenth row.
+  const int b_row = tid >> 1, b_odd = tid & 1, add_row = tid >> 4, add_col = 8 * (tid & 15);
+  const uint32_t b_to = base + (uint32_t)(L::stage0 + b_row * L::row * 2 + b_odd * 16);
+  const uint32_t add_to = base + (uint32_t)(L::add0 + add_row * L::base_row + add_col * 2);
+  int add_adapter[4];
+  const __half* add_from[4];
+#pragma unroll
+  for (int k = 0; k < 4; k++) {
+    const int row = add_row + 16 * k;
+    add_adapter[k] = m0 + row < p.M && p.base && p.wide ? s.adapter[row] : -2;
+    add_from[k] = p.base + (long long)(m0 + row) * p.N + first * kUpCols + add_col;
+  }
+  int b_tile = 0, b_pass = 0, add_tile = 0, add_pass = 0, b_stage = 0, add_stage = 0;
+  auto load_b = [&]() {   // of the next pass
+    if (b_tile < tiles) {
+      const int i = b_pass < different ? s.list[b_pass] : -1, n0 = (first + b_tile) * kUpCols;
+      if (i >= 0 && n0 + b_row < p.N) {
+        const __half* const from = p.b + ((long long)i * p.N + n0 + b_row) * R + 8 * b_odd;
+#pragma unroll
+        for (int q = 0; q < STEPS; q++)
+          if (q < STEPS - 1 || 16 * (STEPS - 1) + 8 * b_odd < R) lora_copy16(b_to + b_stage * L::b_bytes + 32 * q, from + 16 * q);
+      }
+      if (++b_pass == passes) { b_pass = 0; b_tile++; }
+    }
+    b_stage ^= 1;
+  };
+  auto load_add = [&]() {
+    if (add_tile < tiles) {
+      const int i = add_pass < different ? s.list[add_pass] : -1;
+      if ((first + add_tile) * kUpCols + add_col < p.N)
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+          if (add_adapter[k] == i) lora_copy16(add_to + add_stage * L::add_bytes + 16 * k * L::base_row, add_from[k] + add_tile * kUpCols);
+      if (++add_pass == passes) { add_pass = 0; add_tile++; }
+    }
+    if (++add_stage == 3) add_stage = 0;
+  };
+  const int all = tiles * passes;
+  // the rest of an odd number of pieces: never written again
+  for (int v = tid; v < 2 * kUpCols; v += kLoraThreads)
+    *reinterpret_cast<uint4*>(lora_shared + L::stage0 + (v / kUpCols) * L::b_bytes + (v % kUpCols) * L::row * 2 + (STEPS * 16 - 8) * 2) = make_uint4(0, 0, 0, 0);
+  __syncthreads();
+  load_b();
+  load_add();
+  asm volatile("cp.async.commit_group;" ::: "memory");
+  load_b();
+  load_add();
+  load_add();
+  asm volatile("cp.async.commit_group;" ::: "memory");
   // four threads a token: its largest |z|, then z / 2^exponent in two parts, zeroes behind the rank (up to a multiple of 16)
   {
     const int t = tid >> 2, q = tid & 3;
-    const bool have = s.t.adapter[t] >= 0;
+    const bool have = s.adapter[t] >= 0;
     const float* const z = p.z + (long long)(m0 + t) * R;
     float top = 0.f;
     if (have)
@@ -403,126 +472,124 @@ __global__ void __launch_bounds__(kLoraThreads, 2) lora_up_kernel(const LoraPara
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
     const int e = min(max((int)(__float_as_uint(top) >> 23) - 126, -100), 126);   // |z| < 2^e
     const float inv = __int_as_float((127 - e) << 23);
-    if (q == 0) s.unit[t] = __int_as_float((e + 127) << 23);
-    for (int r = 4 * q; r < (R + 15) / 16 * 16; r += 16) {
+    if (q == 0) s_unit[t] = __int_as_float((e + 127) << 23);
+    for (int r = 4 * q; r < STEPS * 16; r += 16) {
       float4 v = have && r < R ? *reinterpret_cast<const float4*>(z + r) : make_float4(0.f, 0.f, 0.f, 0.f);
       v.x *= inv; v.y *= inv; v.z *= inv; v.w *= inv;
       const __half2 h0 = __floats2half2_rn(v.x, v.y), h1 = __floats2half2_rn(v.z, v.w);
       const float2 f0 = __half22float2(h0), f1 = __half22float2(h1);
       const __half2 l0 = __floats2half2_rn(v.x - f0.x, v.y - f0.y), l1 = __floats2half2_rn(v.z - f1.x, v.w - f1.y);
-      *reinterpret_cast<uint2*>(&s.z[0][t][r]) = make_uint2(*reinterpret_cast<const uint32_t*>(&h0), *reinterpret_cast<const uint32_t*>(&h1));
-      *reinterpret_cast<uint2*>(&s.z[1][t][r]) = make_uint2(*reinterpret_cast<const uint32_t*>(&l0), *reinterpret_cast<const uint32_t*>(&l1));
+      // row t % 16 of its 16 tokens, inner elements 4 q .. 4 q + 3: registers 0 and 2 of lane (t % 8) 4 + q, 1 and 3 for the lower eight rows
+      uint32_t* const to = reinterpret_cast<uint32_t*>(lora_shared + ((t >> 4) * STEPS + (r >> 4)) * 512 + ((t & 7) * 4 + q) * 16) + (t >> 3 & 1);
+      constexpr int lower = kLoraTile / 16 * STEPS * 128;   // in words
+      to[0] = *reinterpret_cast<const uint32_t*>(&h0);
+      to[2] = *reinterpret_cast<const uint32_t*>(&h1);
+      to[lower] = *reinterpret_cast<const uint32_t*>(&l0);
+      to[lower + 2] = *reinterpret_cast<const uint32_t*>(&l1);
     }
   }
   __syncthreads();
+  // this thread's four rows: their adapters (-2: no such row), units and places
   const int t0 = (warp >> 2) * 32;
-  constexpr int AHEAD = STEPS < 4 ? STEPS : 4;   // steps whose part of b is asked for at once
-  // this thread's four rows: their adapters (-2: no such row) and places
   int adapter[2][2];
-  long long row[2][2];
+  float unit[2][2];
 #pragma unroll
   for (int m = 0; m < 2; m++)
 #pragma unroll
     for (int h = 0; h < 2; h++) {
       const int t = t0 + m * 16 + h * 8 + g;
-      adapter[m][h] = m0 + t < p.M ? s.t.adapter[t] : -2;
-      row[m][h] = (long long)(m0 + t) * p.N;
+      adapter[m][h] = m0 + t < p.M ? s.adapter[t] : -2;
+      unit[m][h] = s_unit[t];
     }
-  for (int tile = 0; tile < kUpTiles; tile++) {
-    const int n0 = ((int)blockIdx.x * kUpTiles + tile) * kUpCols + (warp & 3) * 32;
-    if (n0 >= p.N) break;
-    const int col = n0 + 8 * j;   // this thread's eight columns
-    const int nb = n0 + 8 * (g >> 1) + (g & 1);
-    // adapter by adapter, the rows that have it; last the rows without any
-    for (int e = 0; e <= different; e++) {
-      const int i = e < different ? s.t.list[e] : -1;
-      bool mine[2][2], any = false;
+  __half* to[2][2];
 #pragma unroll
-      for (int m = 0; m < 2; m++)
+  for (int m = 0; m < 2; m++)
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-          mine[m][h] = adapter[m][h] == i && col < p.N;
-          any |= mine[m][h];
-        }
-      if (!__any_sync(0xffffffffu, any)) continue;
-      uint4 base[2][2];
+    for (int h = 0; h < 2; h++) to[m][h] = p.y + (long long)(m0 + t0 + m * 16 + h * 8 + g) * p.N;
+  const uint8_t* const z0 = lora_shared + (t0 >> 4) * STEPS * 512 + lane * 16;
+  const int b_at = ((warp & 3) * 32 + 8 * (g >> 1) + (g & 1)) * L::row * 2 + 8 * j;                 // column of n-tile 0, and 2 n rows on
+  const int base_at = (t0 + g) * L::base_row + ((warp & 3) * 32 + 8 * j) * 2;
+  int tile = 0, pass = 0, add_now = 0;
+  for (int k = 0; k < all; k++) {
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    __syncthreads();
+    const uint8_t *const st = lora_shared + L::stage0 + (k & 1) * L::b_bytes, *const add_st = lora_shared + L::add0 + add_now * L::add_bytes;
+    const int i = pass < different ? s.list[pass] : -1, col = (first + tile) * kUpCols + (warp & 3) * 32 + 8 * j;
+    bool mine[2][2], any = false;
 #pragma unroll
-      for (int m = 0; m < 2; m++)
+    for (int m = 0; m < 2; m++)
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-          base[m][h] = make_uint4(0, 0, 0, 0);
-          if (mine[m][h] && p.base && p.wide) base[m][h] = *reinterpret_cast<const uint4*>(p.base + row[m][h] + col);
-        }
-      if (i < 0) {   // the row as it is, the signs of its zeroes too
-#pragma unroll
-        for (int m = 0; m < 2; m++)
-#pragma unroll
-          for (int h = 0; h < 2; h++) {
-            if (!mine[m][h]) continue;
-            if (p.wide) *reinterpret_cast<uint4*>(p.y + row[m][h] + col) = base[m][h];
-            else
-              for (int k = 0; k < min(8, p.N - col); k++) p.y[row[m][h] + col + k] = p.base ? p.base[row[m][h] + col + k] : __float2half_rn(0.f);
-          }
-        continue;
+      for (int h = 0; h < 2; h++) {
+        mine[m][h] = adapter[m][h] == i && col < p.N;
+        any |= mine[m][h];
       }
+    if (__any_sync(0xffffffffu, any)) {
       float acc[2][4][4];
+      if (i >= 0) {
+        // fragments of four steps at a time, all asked for in front of the products
+        constexpr int AHEAD = STEPS < 4 ? STEPS : 4;
 #pragma unroll
-      for (int m = 0; m < 2; m++)
+        for (int x0 = 0; x0 < STEPS; x0 += AHEAD) {
+          uint2 bv[AHEAD][4];
+          uint4 a[AHEAD][2];
 #pragma unroll
-        for (int n = 0; n < 4; n++)
+          for (int x = 0; x < AHEAD; x++)
 #pragma unroll
-          for (int k = 0; k < 4; k++) acc[m][n][k] = 0.f;
-      const __half* b[4];
+            for (int n = 0; n < 4; n++)
+              if (x0 + x < STEPS) bv[x][n] = *reinterpret_cast<const uint2*>(st + b_at + 2 * n * L::row * 2 + 32 * (x0 + x));
 #pragma unroll
-      for (int n = 0; n < 4; n++) b[n] = p.b + ((long long)i * p.N + min(nb + 2 * n, p.N - 1)) * R + 4 * j;   // (columns behind the last are dropped)
+          for (int mh = 0; mh < 4; mh++) {   // (upper, lower parts) x (tokens 0 .. 15, 16 .. 31)
+            const int m = mh & 1, h = mh >> 1;
 #pragma unroll
-      for (int k0 = 0; k0 < STEPS; k0 += AHEAD) {
-        uint2 bv[AHEAD][4];
+            for (int x = 0; x < AHEAD; x++)
+              if (x0 + x < STEPS) a[x][mh & 1] = *reinterpret_cast<const uint4*>(z0 + ((h * (kLoraTile / 16) + m) * STEPS + x0 + x) * 512);
 #pragma unroll
-        for (int k = 0; k < AHEAD; k++)
+            for (int x = 0; x < AHEAD; x++)
+              if (x0 + x < STEPS)
 #pragma unroll
-          for (int n = 0; n < 4; n++)
-            if (k0 + k < STEPS)
-              bv[k][n] = k0 + k < STEPS - 1 || 16 * (STEPS - 1) + 4 * j < R ? __ldg(reinterpret_cast<const uint2*>(b[n] + 16 * (k0 + k))) : make_uint2(0, 0);
-#pragma unroll
-        for (int k = 0; k < AHEAD; k++)
-          if (k0 + k < STEPS)
-#pragma unroll
-            for (int m = 0; m < 2; m++)
-#pragma unroll
-              for (int h = 0; h < 2; h++) {
-                const uint2 u = *reinterpret_cast<const uint2*>(&s.z[h][t0 + m * 16 + g][16 * (k0 + k) + 4 * j]);
-                const uint2 v = *reinterpret_cast<const uint2*>(&s.z[h][t0 + m * 16 + 8 + g][16 * (k0 + k) + 4 * j]);
-#pragma unroll
-                for (int n = 0; n < 4; n++) lora_mma(acc[m][n], u.x, v.x, u.y, v.y, bv[k][n].x, bv[k][n].y);
-              }
+                for (int n = 0; n < 4; n++) {
+                  const uint4 u = a[x][mh & 1];
+                  if (x0 + x == 0 && h == 0) lora_mma_first(acc[m][n], u, bv[x][n].x, bv[x][n].y);
+                  else lora_mma(acc[m][n], u.x, u.y, u.z, u.w, bv[x][n].x, bv[x][n].y);
+                }
+          }
+        }
       }
 #pragma unroll
       for (int m = 0; m < 2; m++)
 #pragma unroll
         for (int h = 0; h < 2; h++) {
           if (!mine[m][h]) continue;
-          const float unit = s.unit[t0 + m * 16 + h * 8 + g];
+          __half* const at = to[m][h] + col;
           if (p.wide) {
+            const uint4 add = p.base ? *reinterpret_cast<const uint4*>(add_st + base_at + (m * 16 + h * 8) * L::base_row) : make_uint4(0, 0, 0, 0);
             float v[8];
-            halves8(base[m][h], v);
+            halves8(add, v);
             uint32_t w[4];
 #pragma unroll
             for (int n = 0; n < 4; n++) {
-              const __half2 y = __floats2half2_rn(fmaf(acc[m][n][2 * h], unit, v[2 * n]), fmaf(acc[m][n][2 * h + 1], unit, v[2 * n + 1]));
+              const __half2 y = __floats2half2_rn(fmaf(acc[m][n][2 * h], unit[m][h], v[2 * n]), fmaf(acc[m][n][2 * h + 1], unit[m][h], v[2 * n + 1]));
               w[n] = *reinterpret_cast<const uint32_t*>(&y);
             }
-            *reinterpret_cast<uint4*>(p.y + row[m][h] + col) = make_uint4(w[0], w[1], w[2], w[3]);
+            // (without an adapter the row as it is, the signs of its zeroes too)
+            *reinterpret_cast<uint4*>(at) = i < 0 ? add : make_uint4(w[0], w[1], w[2], w[3]);
           } else {
+            const __half* const add = p.base ? p.base + (at - p.y) : nullptr;
 #pragma unroll
-            for (int k = 0; k < 8; k++)
-              if (col + k < p.N) {
-                const long long at = row[m][h] + col + k;
-                p.y[at] = __float2half_rn(fmaf(acc[m][k >> 1][2 * h + (k & 1)], unit, p.base ? __half2float(p.base[at]) : 0.f));
+            for (int x = 0; x < 8; x++)
+              if (col + x < p.N) {
+                const float v = add ? __half2float(add[x]) : 0.f;
+                at[x] = __float2half_rn(i < 0 ? v : fmaf(acc[m][x >> 1][2 * h + (x & 1)], unit[m][h], v));
               }
           }
         }
     }
+    __syncthreads();
+    load_b();
+    load_add();
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    if (++add_now == 3) add_now = 0;
+    if (++pass == passes) { pass = 0; tile++; }
   }
 }
 
