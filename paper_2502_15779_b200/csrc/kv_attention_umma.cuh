@@ -336,9 +336,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
           if (ok && t + 1 < tiles) tile(t + 1, sb, sa);
         }
       }
-      // (one after the other: a wait by parity is good for the phase behind one that is known to be over)
-      if (ok && tiles > 1) ok = prompt_wait(o_done + 8 * half, (tiles - 2) & 1);
-      if (ok && tiles > 0) ok = prompt_wait(o_done + 8 * half, (tiles - 1) & 1);
+      // All products are done. (Not a wait for the last phase of o_done: that one may be over before the one in front of it is waited for.)
+      if (ok) ok = prompt_wait(drained + 8 * half, 0);
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       if (ok) {
         __half* const to = p.out + ((long long)(sq.t0 + i) * p.heads + (long long)kv * p.group + (r - i * p.group)) * DIM;

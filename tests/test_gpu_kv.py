@@ -304,6 +304,21 @@ def test_attention_of_many_ctas_at_once(dim, heads, new, length):
     assert all(torch.equal(o, outs[0]) for o in outs[1:])
 
 
+@pytest.mark.parametrize("new,cached,heads,kv_heads,dim", [([300], [129], 12, 4, 64), ([65, 1, 129], [3, 50, 200], 8, 2, 128), ([70], [0], 4, 1, 128)])
+def test_attention_of_short_prompts_many_times(new, cached, heads, kv_heads, dim):
+    """A few tiles of keys, whose ends the kernel's warps reach in any order: no wait may give up and every run gives the same."""
+    page, lengths = 64, [n + c for n, c in zip(new, cached)]
+    pages = sum(-(-n // page) for n in lengths) + 1
+    cache = random_cache(pages, kv_heads, page, dim, seed=68)
+    args = tensors(starts_of(new), lengths, make_table(lengths, page, pages, seed=69))
+    q, ws = rand(sum(new), heads, dim, seed=70), rcp.make_kv_workspace(DEV)
+    first = rcp.rcp_kv_attention(q, cache, *args, workspace=ws)
+    bad = torch.zeros((), dtype=torch.int64, device=DEV)
+    for _ in range(400):
+        bad += (rcp.rcp_kv_attention(q, cache, *args, workspace=ws) != first).sum()
+    assert int(ws[:4].view(torch.int32)) == 0 and int(bad) == 0
+
+
 def test_captured_calls_follow_lengths_and_tables():
     """Append and attention of a decode step captured once; lengths and tables change between replays."""
     page, dim, heads, kv_heads, B = 32, 64, 8, 2, 3
