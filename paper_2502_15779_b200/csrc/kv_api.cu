@@ -68,11 +68,11 @@ int attn_split(const rcp::AttnParams& p, cudaStream_t st) {
   return RCP_OK;
 }
 
-// Rows of a sequence (new tokens x query heads of a key head) up to which the split kernel takes it: one row tile of it where the
-// prompt kernel's CTAs, one a key head and sequence, fill the GPU without a split along the keys, three otherwise. Measured, split against
-// prompt kernel, us, 8 key heads: 16 sequences x 32 rows x 4000 keys 69 : 25, x 64 rows 91 : 27; 8 x 48 x 8000 61 : 90; 4 x 64 x 4000
-// 36 : 60; 2 x 64 x 30000 78 : 314.
-int attn_few_rows(int seqs, int kv_heads) { return (int64_t)seqs * kv_heads >= 2 * sm_count() / 3 ? rcp::kAttnMaxRows : 64; }
+// Rows of a sequence (new tokens x query heads of a key head) up to which the split kernel takes it: two row tiles of it where the prompt
+// kernel's CTAs, one a key head and sequence, fill the GPU without a split along the keys, nearly three otherwise. Measured, split against
+// prompt kernel, us, 8 key heads, 4000 keys: 16 sequences x 32 rows 69 : 72, x 64 rows 91 : 74; 64 x 32 190 : 226, 64 x 64 257 : 216; 4 x 64
+// 36 : 60; 2 x 64 x 30000 keys 78 : 480; 8 x 48 x 8000 61 : 135.
+int attn_few_rows(int seqs, int kv_heads) { return (int64_t)seqs * kv_heads >= 2 * sm_count() / 3 ? 2 * rcp::kAttnMaxRows : 64; }
 
 template <int DIM>
 int attn_prompt(const rcp::AttnParams& p, cudaStream_t st) {

@@ -38,17 +38,20 @@ __device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t (&r)[32]) {
         "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(at) : "memory");
 }
-__device__ __forceinline__ void tmem_ld16(uint32_t at, uint32_t (&r)[16]) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-                 "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-               : "r"(at) : "memory");
-}
 __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at), "r"(r[0]),
                "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
                "r"(r[13]), "r"(r[14]), "r"(r[15])
                : "memory");
+}
+__device__ __forceinline__ void tmem_st32w(uint32_t at, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(at),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+      "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
+      "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
 }
 // fp32 += fp16 x fp16; A from shared memory or from tensor memory (at `a`)
 __device__ __forceinline__ void umma_ss(uint32_t elected, uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t acc) {
@@ -84,8 +87,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 // Pages and scales of a sequence's keys in units of 32, one unit a lane, 32 units (sixteen tiles) at a time; the next 32 are asked for ahead.
-// And the unit of the sums, a power of two: four above the largest exponent among the first 32 units' values, and moved to four above a
-// tile's largest one when that is not within -11 .. 7 of it. As a rule all 32 are, and a tile costs no more than a look at `calm`.
 struct PromptBlocks {
   const KvSeqs* s;
   const int32_t* row;                 // the sequence's row of the table
@@ -93,9 +94,8 @@ struct PromptBlocks {
   int kv, kv_heads, end, lane;
   int page, next_page;                // -1: none
   float ks, next_ks;
-  int ve, next_ve;                    // exponent of the values' scale, INT_MIN without a page
-  int unit;                           // exponent of the unit of the sums
-  bool calm;                          // it does not move within these 32
+  int ve, next_ve;                    // exponent of the values' scale
+  int unit;                           // exponent of the unit of the sums; INT_MIN in front of the first tile
 
   __device__ __forceinline__ int find(int at) const {   // page of keys 32 at ..
     if (at * 32 >= end) return -1;
@@ -103,29 +103,26 @@ struct PromptBlocks {
     return pg >= 0 && pg < s->pages ? pg : -1;
   }
   __device__ __forceinline__ void scales(int pg, float& k, int& v) const {
-    k = pg >= 0 ? k_scale[(long long)pg * kv_heads + kv] : 0.f;
+    k = pg >= 0 ? k_scale[(long long)pg * kv_heads + kv] : 1.f;
     v = pg >= 0 ? kv_stored_exponent(v_scale[(long long)pg * kv_heads + kv]) : INT_MIN;
   }
   __device__ __forceinline__ void start() {
     next_page = find(lane);
     scales(next_page, next_ks, next_ve);
-    const int top = __reduce_max_sync(0xffffffffu, next_ve);
-    unit = top == INT_MIN ? 0 : top + 4;
+    unit = INT_MIN;
   }
-  // To be called for every tile in turn, up front; returns by how many powers of two the sums' unit grows with it.
+  // to be called for every tile in turn; returns by how many powers of two the sums' unit grows with it (0 as a rule)
   __device__ __forceinline__ int step(int tile) {
     if ((tile & 15) == 0) {
       page = next_page; ks = next_ks; ve = next_ve;
       next_page = find((tile + 16) * 2 + lane);
-      calm = __all_sync(0xffffffffu, ve == INT_MIN || (ve - unit <= 7 && ve - unit >= -11));
     }
     if ((tile & 15) == 8) scales(next_page, next_ks, next_ve);
-    if (calm) return 0;
-    const int at = (tile & 15) * 2, top = max(__shfl_sync(0xffffffffu, ve, at), __shfl_sync(0xffffffffu, ve, at + 1));
-    if (top == INT_MIN || (top - unit <= 7 && top - unit >= -11)) return 0;   // (no keys in this tile)
-    const int grow = top + 4 - unit;
+    const int at = (tile & 15) * 2, a = __shfl_sync(0xffffffffu, ve, at), b = __shfl_sync(0xffffffffu, ve, at + 1), top = max(a, b);
+    if (top == INT_MIN) return 0;                       // no keys in this tile
+    if (unit != INT_MIN && top - unit <= 7 && top - unit >= -11) return 0;
+    const int grow = unit == INT_MIN ? 0 : top + 4 - unit;
     unit = top + 4;
-    calm = __all_sync(0xffffffffu, ve == INT_MIN || (ve - unit <= 7 && ve - unit >= -11));
     return grow;
   }
 };
@@ -170,16 +167,16 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
   const uint32_t o_done = p_full + 32, drained = o_done + 16;                        // [row tile]
   if (tid == 0) {
     for (uint32_t i = 0; i < STAGES; i++) {
-      mbar_init(k_full + 8 * i, 4);   // (an arrival a warp: 128 of them took longer than the products)
+      mbar_init(k_full + 8 * i, 128);
       mbar_init(k_empty + 8 * i, halves);
-      mbar_init(v_full + 8 * i, 4);
+      mbar_init(v_full + 8 * i, 128);
       mbar_init(v_empty + 8 * i, halves);
     }
     for (int i = 0; i < 2; i++) {
       mbar_init(s_full + 16 * i, 1);
       mbar_init(s_full + 16 * i + 8, 1);
-      mbar_init(p_full + 16 * i, 4);
-      mbar_init(p_full + 16 * i + 8, 4);
+      mbar_init(p_full + 16 * i, 128);
+      mbar_init(p_full + 16 * i + 8, 128);
       mbar_init(o_done + 8 * i, 1);
       mbar_init(drained + 8 * i, 1);
     }
@@ -225,56 +222,41 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
       const int least = (int)__reduce_min_sync(0xffffffffu, lim);
       float m = kAttnNoMax, l = 0.f;
       blocks.start();
-      // factors of the next tile's scores, zero where there are no keys, and what its unit grows by: made while the exponentials are
-      float next_c[2], next_top = -INFINITY;
-      int next_grow;
-      auto ahead = [&](int t) {
-        next_grow = blocks.step(t);
+      for (int t = 0; t < tiles; t++) {
+        const int grow = blocks.step(t);
+        float c[2];
+        bool some = true;
 #pragma unroll
         for (int k = 0; k < 2; k++) {
-          const float ks = __shfl_sync(0xffffffffu, blocks.ks, (t & 15) * 2 + k);
-          next_c[k] = ks > 0.f ? fmaxf(ks * p.scale_log2, 1e-37f) : 0.f;   // above zero: a score of -inf stays one
+          const int from = (t & 15) * 2 + k;
+          c[k] = fmaxf(__shfl_sync(0xffffffffu, blocks.ks, from) * p.scale_log2, 1e-37f);   // above zero: a score of -inf stays one
+          some = some && __shfl_sync(0xffffffffu, blocks.page, from) >= 0;
         }
-      };
-      // scores of tile t on their way to registers (stale ones behind the last tile: nothing comes of them)
-      auto ask = [&](int t, uint32_t (&s)[2][32]) {
-        if (t < tiles) ok = prompt_wait(s_full + 16 * half + 8 * (t & 1), (uint32_t)(t >> 1) & 1u);
+        const uint32_t at = at_s + 64u * (t & 1);
+        ok = prompt_wait(s_full + 16 * half + 8 * (t & 1), (uint32_t)(t >> 1) & 1u);
+        if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        tmem_ld32(at_s + 64u * (t & 1), s[0]);
-        tmem_ld32(at_s + 64u * (t & 1) + 32u, s[1]);
-      };
-      auto hide = [&](int t, uint32_t (&s)[2][32]) {   // keys that the row does not see, or that are not there
-        if (next_c[0] * next_c[1] == 0.f || (t + 1) * kPromptKeys > least) {
+        uint32_t s[2][32];
+        tmem_ld32(at, s[0]);
+        tmem_ld32(at + 32u, s[1]);
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        if (!some || (t + 1) * kPromptKeys > least) {   // keys that some row of the warp does not see, or that are not there
 #pragma unroll
           for (int k = 0; k < 2; k++) {
-            const int left = next_c[k] > 0.f ? lim - t * kPromptKeys - 32 * k : 0;
+            const int left = __shfl_sync(0xffffffffu, blocks.page, (t & 15) * 2 + k) >= 0 ? lim - t * kPromptKeys - 32 * k : 0;
 #pragma unroll
             for (int x = 0; x < 32; x++)
               if (x >= left) s[k][x] = 0xFF800000u;
           }
         }
-      };
-      auto largest = [&](const uint32_t (&s)[2][32]) {
-        float a[2][4];
+        float top = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < 2; k++)
+        for (int k = 0; k < 2; k++) {
+          float a[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int x = 0; x < 4; x++) a[k][x] = __uint_as_float(s[k][x]);
-#pragma unroll
-        for (int x = 4; x < 32; x += 8)
-#pragma unroll
-          for (int k = 0; k < 2; k++)
-#pragma unroll
-            for (int y = 0; y < 4; y++)
-              a[k][y] = x + 4 + y < 32 ? max3(a[k][y], __uint_as_float(s[k][x + y]), __uint_as_float(s[k][x + 4 + y])) : fmaxf(a[k][y], __uint_as_float(s[k][x + y]));
-        // (a factor of zero: every score is -inf)
-        next_top = fmaxf(next_c[0] > 0.f ? max3(fmaxf(a[0][0], a[0][1]), a[0][2], a[0][3]) * next_c[0] : -INFINITY,
-                         next_c[1] > 0.f ? max3(fmaxf(a[1][0], a[1][1]), a[1][2], a[1][3]) * next_c[1] : -INFINITY);
-      };
-      // Tile t, whose scores are in s; those of the next one come to `sn` meanwhile, and their maximum is found between the exponentials.
-      auto tile = [&](int t, uint32_t (&s)[2][32], uint32_t (&sn)[2][32]) {
-        const int grow = next_grow;
-        const float top = next_top;
+          for (int x = 0; x < 16; x++) a[x & 3] = max3(a[x & 3], __uint_as_float(s[k][2 * x]), __uint_as_float(s[k][2 * x + 1]));
+          top = fmaxf(top, max3(fmaxf(a[0], a[1]), a[2], a[3]) * c[k]);
+        }
         if (__any_sync(0xffffffffu, top > m + kAttnSlack || grow != 0)) {
           const float mn = fmaxf(m, top), f = exp2_fast(m - mn);
           m = mn;
@@ -282,61 +264,39 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
           const float fu = f * kv_pow2(min(max(-grow, -100), 100));
           if (t > 0) {
             ok = prompt_wait(o_done + 8 * half, (t - 1) & 1);   // the product of the tile in front is in the sums
-            if (!ok) return;
+            if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-#pragma unroll 1
-            for (int d = 0; d < DIM / 16; d++) {
-              uint32_t o[16];
-              tmem_ld16(at_o + 16u * d, o);
+#pragma unroll
+            for (int d = 0; d < DIM / 32; d++) {
+              uint32_t o[32];
+              tmem_ld32(at_o + 32u * d, o);
               asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-              for (int x = 0; x < 16; x++) o[x] = __float_as_uint(__uint_as_float(o[x]) * fu);
-              tmem_st16(at_o + 16u * d, o);
+              for (int x = 0; x < 32; x++) o[x] = __float_as_uint(__uint_as_float(o[x]) * fu);
+              tmem_st32w(at_o + 32u * d, o);
             }
           }
         }
-        const float ref = m - kAttnLift, f[2] = {next_c[0] > 0.f ? next_c[0] : 1.f, next_c[1] > 0.f ? next_c[1] : 1.f};
+        const float ref = m - kAttnLift;
         float2 sum[2] = {};
-        auto weights = [&](int k) {
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
           uint32_t w[16];
 #pragma unroll
           for (int x = 0; x < 16; x++) {
-            const float2 y = fma2(make_float2(__uint_as_float(s[k][2 * x]), __uint_as_float(s[k][2 * x + 1])), make_float2(f[k], f[k]), make_float2(-ref, -ref));
+            const float2 y = fma2(make_float2(__uint_as_float(s[k][2 * x]), __uint_as_float(s[k][2 * x + 1])), make_float2(c[k], c[k]), make_float2(-ref, -ref));
             const float2 e = make_float2(exp2_fast(y.x), exp2_fast(y.y));
             const __half2 h = __float22half2_rn(e);
             w[x] = *reinterpret_cast<const uint32_t*>(&h);
             sum[x & 1] = add2(sum[x & 1], e);
           }
-          tmem_st16(at_s + 64u * (t & 1) + 16u * k, w);
-        };
-        if (t + 1 < tiles) ahead(t + 1);
-        ask(t + 1, sn);
-        if (!ok) return;
-        weights(0);
-        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-        hide(t + 1, sn);
-        largest(sn);
-        weights(1);
+          tmem_st16(at + 16u * k, w);
+        }
         l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(p_full + 16 * half + 8 * (t & 1));
-      };
-      if (tiles > 0) {
-        uint32_t sa[2][32], sb[2][32];
-        ahead(0);
-        ask(0, sa);
-        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-        hide(0, sa);
-        largest(sa);
-#pragma unroll 1
-        for (int t = 0; t < tiles && ok; t += 2) {
-          tile(t, sa, sb);
-          if (ok && t + 1 < tiles) tile(t + 1, sb, sa);
-        }
+        mbar_arrive(p_full + 16 * half + 8 * (t & 1));
       }
-      // All products are done. (Not a wait for the last phase of o_done: that one may be over before the one in front of it is waited for.)
       if (ok) ok = prompt_wait(drained + 8 * half, 0);
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       if (ok) {
@@ -438,15 +398,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
       if (!ok) break;
       put(codes[0], base + L::k + stage * L::tile_bytes, false, now);
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive(k_full + 8 * stage);
+      mbar_arrive(k_full + 8 * stage);
       if (t + 1 < tiles) ask(codes[0], p.k_cache);
       ok = prompt_wait(v_empty + 8 * stage, parity ^ 1u);
       if (!ok) break;
       put(codes[1], base + L::v + stage * L::tile_bytes, true, now);
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive(v_full + 8 * stage);
+      mbar_arrive(v_full + 8 * stage);
       if (t + 1 < tiles) ask(codes[1], p.v_cache);
     }
   } else {
