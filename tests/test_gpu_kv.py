@@ -272,6 +272,75 @@ def test_attention_of_more_tokens_than_max_new_leaves_the_rest():
     check_attention(rcp.rcp_kv_attention(q, cache, *tensors(starts, lengths, table), sm_scale=0.1, max_new=20, out=out), want, tol)
 
 
+def test_attention_of_many_short_sequences():
+    """More sequences than a CTA has threads, some without new tokens or without any tokens, few rows and many among them."""
+    page, dim, heads, kv_heads, B = 32, 64, 8, 4, 700
+    g = torch.Generator().manual_seed(55)
+    new = (torch.rand(B, generator=g) * 3).int().tolist()
+    new[5], new[300], new[699] = 150, 40, 60
+    lengths = [n + int(x) for n, x in zip(new, (torch.rand(B, generator=g) * 90).int())]
+    lengths[0] = new[0] = 0
+    pages = sum(-(-n // page) for n in lengths)
+    cache = random_cache(pages, kv_heads, page, dim, seed=56)
+    table = make_table(lengths, page, pages, seed=57)
+    starts = starts_of(new)
+    q = rand(sum(new) + 2, heads, dim, seed=58)
+    want, tol = ref.attention(q, cache, starts, lengths, table, dim ** -0.5)
+    out = torch.full(q.shape, math.nan, dtype=torch.float16, device=DEV)
+    check_attention(rcp.rcp_kv_attention(q, cache, *tensors(starts, lengths, table), out=out), want, tol)
+    # one token each: the kernel of few rows alone
+    new, starts = [1] * B, starts_of([1] * B)
+    q = rand(B, heads, dim, seed=59)
+    lengths = [max(n, 1) for n in lengths]
+    table = make_table(lengths, page, pages + B, seed=60)
+    cache = random_cache(pages + B, kv_heads, page, dim, seed=61)
+    want, tol = ref.attention(q, cache, starts, lengths, table, dim ** -0.5)
+    check_attention(rcp.rcp_kv_attention(q, cache, *tensors(starts, lengths, table), max_new=1), want, tol)
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(40, 1), (200, 1), (64, 1), (65, 1), (128, 2), (3, 3)])
+@pytest.mark.parametrize("new", [1, 3])
+def test_attention_many_query_heads_of_a_key_head(heads, kv_heads, new):
+    page, dim, lengths = 64, 128, [500, 64, 131]
+    cache = random_cache(13, kv_heads, page, dim, seed=44)
+    table = make_table(lengths, page, 13, seed=45)
+    q = rand(3 * new, heads, dim, seed=46)
+    for seqs in (1, 3):
+        starts = starts_of([new] * seqs)
+        want, tol = ref.attention(q[:seqs * new], cache, starts, lengths[:seqs], table[:seqs], dim ** -0.5)
+        check_attention(rcp.rcp_kv_attention(q[:seqs * new], cache, *tensors(starts, lengths[:seqs], table[:seqs]), max_new=new), want, tol)
+
+
+@pytest.mark.parametrize("new", [1, 9, 100])
+def test_attention_a_bad_query_stays_alone_and_a_scale_of_zero_weighs_all_alike(new):
+    page, dim, heads, kv_heads, n = 64, 64, 8, 2, 400
+    cache = random_cache(8, kv_heads, page, dim, seed=47)
+    table = make_table([n], page, 8, seed=48)
+    args = tensors([0, new], [n], table)
+    q = rand(new, heads, dim, seed=49)
+    want, tol = ref.attention(q, cache, [0, new], [n], table, dim ** -0.5)
+    q[0, 1, 3], q[new // 2, 6, 0], q[new - 1, 7, 9] = math.nan, math.inf, math.nan
+    got = rcp.rcp_kv_attention(q, cache, *args)
+    fine = torch.ones(new, heads, dtype=torch.bool, device=DEV)
+    for t, h in ((0, 1), (new // 2, 6), (new - 1, 7)):
+        fine[t, h] = False
+    assert bool(((got.double() - want).abs() <= tol)[fine].all())
+    assert bool(torch.isnan(got[0, 1]).all()) and bool(torch.isnan(got[new - 1, 7]).all())
+    q = rand(new, heads, dim, seed=50)
+    check_attention(rcp.rcp_kv_attention(q, cache, *args, sm_scale=0.0), *ref.attention(q, cache, [0, new], [n], table, 0.0))
+
+
+def test_attention_in_the_place_of_its_queries():
+    page, dim, heads, kv_heads = 64, 128, 8, 2
+    for new, length in ((1, 5000), (150, 700)):
+        cache = random_cache(90, kv_heads, page, dim, seed=51)
+        table = make_table([length], page, 90, seed=52)
+        args = tensors([0, new], [length], table)
+        q = rand(new, heads, dim, seed=53)
+        want = rcp.rcp_kv_attention(q.clone(), cache, *args)
+        assert torch.equal(rcp.rcp_kv_attention(q, cache, *args, out=q), want)
+
+
 def test_attention_results_repeat_and_leave_the_workspace_ready():
     page, dim, heads, kv_heads = 64, 128, 16, 2
     lengths = [5000, 1, 900, 12000]

@@ -61,6 +61,45 @@ def test_requests_in_order_strided_rows_and_no_adapters(M):
         check(rcp.rcp_lora_add(wide[:, 8:520], a, b, adapter, scaling, base=base), want, tol)
 
 
+@pytest.mark.parametrize("M,N", [(3, 512), (100, 512), (130, 77)])
+def test_results_that_start_between_sixteen_bytes(M, N):
+    x, a, b, adapter, scaling, base = case(M, N, 256, 16, 3, seed=31)
+    odd = [torch.empty(M * N + 1, dtype=torch.float16, device=DEV)[1:].view(M, N) for _ in range(2)]
+    odd[0].copy_(base)
+    want, tol = ref.lora(x, a, b, adapter, scaling, base)
+    check(rcp.rcp_lora_add(x, a, b, adapter, scaling, base=odd[0], y=odd[1]), want, tol)
+    check(rcp.rcp_lora_add(x, a, b, adapter, scaling, base=base, y=odd[1]), want, tol)
+    check(rcp.rcp_lora_add(x, a, b, adapter, scaling, base=odd[0], y=odd[0]), want, tol)
+
+
+def test_a_large_token_beside_a_small_one():
+    """z of the prompt form is scaled a token: large and tiny activations side by side, sums beyond fp16's range."""
+    M, N, K, R = 80, 200, 512, 32
+    x, a, b, adapter, scaling, _ = case(M, N, K, R, 2, seed=33)
+    x[::3] *= 2000.0
+    x[1::3] *= 1e-4
+    a *= 30.0
+    b *= 1e-3
+    want, tol = ref.lora(x, a, b, adapter, scaling, None)
+    check(rcp.rcp_lora_add(x, a, b, adapter, scaling), want, tol)
+
+
+def test_calls_on_several_streams():
+    sets = []
+    for i, (M, N) in enumerate(((1, 4096), (16, 1000), (200, 700))):
+        args = case(M, N, 1024, 16, 4, seed=60 + i)
+        sets.append((args, rcp.rcp_lora_add(*args[:5], base=args[5]), rcp.make_lora_workspace(M, 16, DEV), torch.empty(M, N, dtype=torch.float16, device=DEV),
+                     torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for args, _, ws, y, st in sets:
+            with torch.cuda.stream(st):
+                rcp.rcp_lora_add(*args[:5], base=args[5], y=y, workspace=ws)
+    torch.cuda.synchronize()
+    for _, want, _, y, _ in sets:
+        assert torch.equal(y, want)
+
+
 def test_a_bad_number_stays_with_its_token():
     """NaN and infinity in one token's activations or one adapter's weights reach no other token, and a token without an adapter keeps
     its base bit for bit."""
