@@ -456,8 +456,8 @@ int rcp_selftest_wait_timeout(void* workspace, int polls, void* stream);
  * A block whose first slot is among the new tokens gets the smallest scale 2^e with max |x| <= 448 2^e over its new tokens;
  * one that holds older tokens keeps its scale unless it has to grow, and then its older codes are rounded to the new
  * scale. Codes: round to nearest even. Slots behind the last token are left as they were. A NaN is stored as zero,
- * magnitudes above 2^17 as 2^17. Pages that get new tokens belong to one sequence each (two that share one race on its
- * contents; sequences may share pages that none of them appends to).
+ * magnitudes above 2^17 as 2^17. Pages that get new tokens belong to one sequence each, in one place (two that share one race
+ * on its contents; sequences may share pages that none of them appends to).
  * Asynchronous on `stream`; allocates nothing, needs no workspace.
  */
 int rcp_kv_append(const void* q_f16, int64_t q_stride, const void* k_f16, int64_t k_stride, const void* v_f16, int64_t v_stride,
@@ -471,12 +471,16 @@ int rcp_kv_append(const void* q_f16, int64_t q_stride, const void* k_f16, int64_
  *   out[t][h] = sum_j p_j v_j / sum_j p_j,  p_j = exp(sm_scale * (q[t][h] . k_j)),  kv head h / (heads / kv_heads)
  *   q          fp16 [tokens][heads][dim], rows q_stride elements apart as for rcp_kv_append, rotated already.
  *   sm_scale   finite, >= 0 (as a rule 1/sqrt(dim)).
- *   out        fp16 [tokens][heads][dim], without gaps, 16-byte aligned. A row without keys (an empty sequence, no pages) is
- *              zero; rows of no sequence are left as they were.
+ *   out        fp16 [tokens][heads][dim], without gaps, 16-byte aligned; may be q itself if q has no gaps. A row without keys
+ *              (an empty sequence, no pages) is zero; rows of no sequence are left as they were.
  *   workspace  rcp_kv_attention_workspace_bytes() bytes, 16-byte aligned, zero-filled once; every call leaves it ready
- *              for the next. Calls that may overlap on the GPU need one each.
+ *              for the next. Calls that may overlap on the GPU need one each. Its first word receives a non-zero code if one of
+ *              the bounded waits of the kernel for many rows gives up (3: softmax, 4: conversion, 5: issue; 0 otherwise): the
+ *              results of that call are then invalid, and so are those of later calls until the buffer is zero-filled again.
  * Nothing behind a sequence's length is read: slots that were never written may hold anything.
- * Scores, maxima and sums in fp32; weights are rounded to fp16 for the product with the values, sums stay in fp32.
+ * Scores, maxima and sums in fp32; weights are rounded to fp16 for the product with the values, sums stay in fp32. In the kernel
+ * for many rows values go through fp16 relative to the largest scale of their 64 positions: exact within 2^11 of it, nothing
+ * is left at 2^20.
  * Asynchronous on `stream`; allocates nothing.
  */
 size_t rcp_kv_attention_workspace_bytes(void);
@@ -490,8 +494,8 @@ int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads,
  * other): token m uses adapter i = adapter[m],
  *   y[m][n] = fp16( base[m][n] + scaling[i] * sum_r b[i][n][r] * (sum_k a[i][r][k] * x[m][k]) )       (fp32 arithmetic)
  *   x        fp16 [M][K], rows x_stride elements apart (a multiple of 8, at least K); 16-byte aligned. K % 64 == 0.
- *   a, b     fp16 [adapters][rank][K] and [adapters][N][rank], 16-byte aligned; rank a multiple of 8 up to
- *            RCP_LORA_MAX_RANK (fill a smaller adapter up with zeros).
+ *   a, b     fp16 [adapters][rank][K] and [adapters][N][rank], 16-byte aligned, constants like a layer's weights; rank a
+ *            multiple of 8 up to RCP_LORA_MAX_RANK (fill a smaller adapter up with zeros).
  *   adapter  int32 [M]; an entry outside 0 .. adapters - 1: none, y is base.
  *   scaling  fp32 [adapters].
  *   base     fp16 [M][N], the projection's output; NULL: zero. May be y (the adapters are added in place).

@@ -1,5 +1,6 @@
 """B200-native (sm_100a) library for the decode-time W2A4 hot path of RCP (arXiv 2502.15779):
-weight-code packing, fused Hadamard + int4 activation quantization, and the LUT GEMV.
+weight-code packing, fused Hadamard + int4 activation quantization, and the LUT GEMV; beside them a paged 8-bit cache of keys and
+values, attention over it and low-rank adapters of many requests.
 
 The compute lives in ``librcp_w2a4.so`` (hand-written CUDA behind the C ABI of include/rcp.h);
 this package only marshals arguments. Importing it needs neither a GPU nor the built library;

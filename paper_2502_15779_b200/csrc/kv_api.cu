@@ -94,7 +94,7 @@ int lora_up(rcp::LoraParams p, int tiles, cudaStream_t st) {
   static bool done[kMaxDevices] = {};
   RCP_CUDA(set_max_smem(rcp::lora_up_kernel<STEPS>, L::bytes, mu, done));
   // Column tiles of a CTA: few waves of CTAs, and short ones, because tiles in which tokens of two requests meet take twice as long (2011 tokens of
-  // six requests, 28672 columns: 8 tiles a CTA, whose fourth wave is all but empty, 105 us a call; one wave of 25 tiles 146; 5 tiles RESULT).
+  // six requests, 28672 columns, us a call: 3 tiles a CTA 113, 5 (the choice) 106, 8 105, 13 116, one wave of 25 tiles 135).
   const int cols = (p.N + rcp::kUpCols - 1) / rcp::kUpCols, at_once = sm_count() * std::min<int>(3, 232448 / (L::bytes + 2048));
   double least = 0;
   for (int n = 1; n <= std::min(cols, 16); n++) {

@@ -1,17 +1,24 @@
 // Attention of many rows of a sequence (prompts, long guesses) over the paged 8-bit cache on tcgen05; the operator is that of
 // kv_attention.cuh, for the sequences whose new tokens times query heads of a key head are more than p.few.
 //
-// Bound by the tensor cores and by the exponentials beside them (one for every row and key, 16 a clock and SM).
 // Work. One CTA a key head and 256 rows of a sequence (tokens x query heads that share the key head, token by token), two row tiles of 128.
-// For each tile of 128 keys: S_t = Q_t K^T (both operands in shared memory), weights to tensor memory as fp16 in the place of the scores,
-// O_t += P_t V (weights from tensor memory). Scores and sums of both row tiles fill tensor memory: 2 (128 + dim) columns.
+// For each tile of 64 keys: S_t = Q_t K^T (both operands in shared memory), weights to tensor memory as fp16 in the place of the scores,
+// O_t += P_t V (weights from tensor memory). Tensor memory is full: for each row tile two tiles of scores and the sums, 2 x 64 + dim columns.
 // Warps. Four that turn codes into fp16, once for all 256 rows, from memory through registers into shared memory (128-byte
-// swizzle; values keep their order, keys along the rows, and are read as a transposed operand); two that issue, one a row tile, so that neither waits for the
-// other's softmax; eight for the softmax, one thread a row. While one row tile's weights are made, the tensor cores work on the other.
+// swizzle; values keep their order, keys along the rows, and are read as a transposed operand); two that issue, one a row tile, so that neither
+// waits for the other's softmax; eight for the softmax, one thread a row. The next tile's scores are made while the softmax works on these.
 // Softmax as in kv_attention.cuh: a row's reference moves only when a score is more than kAttnSlack above it, the sums in tensor memory
-// are rescaled then. The scales of the values' blocks are folded into the fp16 values relative to a power of two, the unit of the
-// sums, which stays while every block's exponent is within -11 .. 7 of it (fp16 then holds all codes exactly) and moves otherwise; converters
-// and softmax warps follow the same rule on the same scales, so nothing has to be handed over.
+// are rescaled then. (The sum of the weights is of fp32 ones here: tensor memory has no column left for it.) The scales of the values' blocks
+// are folded into the fp16 values relative to a power of two, the unit of the sums, which stays while a tile's largest exponent is within
+// -11 .. 7 of it (fp16 then holds that block's codes exactly) and moves to four above it otherwise; converters and softmax warps follow the same rule on
+// the same scales, so nothing has to be handed over. (A block whose scale is more than 2^11 below that of another one in the same 64 keys loses
+// low bits of its smallest codes, one 2^20 below all of them.)
+// Bound by the softmax warps' chain of a tile: of 2250 clocks factors and masks take 380, the wait for the scores 195, reading them 87, their
+// maximum 470, exponentials, sums and fp16 1090; the tensor pipe is at work 1280 of them (64 keys of both row tiles; the scores' products are
+// bound by shared memory, 48 clocks each instead of 32), the exponentials' unit 1024. 32 heads on 8, prompts of 2000, 1790 and 1190 tokens behind
+// 3000, 2506 and 2154: 340 us, 836 TFLOP/s; 17 % of it is the last wave of CTAs. Steps: tiles of 128 keys with one tile of scores 446 us; with the 128
+// scores of a row in registers at once (spilled) 529; the next scores read between the exponentials 429 (they are waited for a whole chain too
+// early: the place they go to is free only when the weights in it have been multiplied).
 #pragma once
 #include "kv_attention.cuh"
 #include "ptx.cuh"

@@ -3,13 +3,16 @@
 //
 // lora_few_kernel: up to kLoraFew tokens, as in decoding. Bound by latency, and by the adapters' bytes where every token has its own. One
 // launch: a cluster of eight CTAs takes the tokens of one adapter (eight at most), each CTA a part of K for z; the parts of z go to
-// all eight through distributed shared memory, and behind the cluster's barrier each CTA takes a part of the rows of b.
+// all eight through distributed shared memory, and behind the cluster's barrier each CTA takes a part of the rows of b. One token, 10240 x 8192, rank
+// 16: 4.4 us (two launches: 15 with a plain loop a row); sixteen tokens of up to sixteen adapters, 6144 x 4096, rank 32: 6.7 us, 1.6 TB/s.
 // lora_down_kernel, lora_up_kernel: more tokens, as in prompts, in tiles; bound by x, base and y (with hundreds of tokens an
 // adapter is read from L2). Both products on the tensor cores, fragments straight from memory: the order of the inner index
 // is free as long as both operands share it, so a thread reads 16 (z) or 8 (y) contiguous bytes. z is a sum in fp32; for the second
 // product each token's row is scaled by a power of two and split into two fp16 numbers, 22 bits of it. A tile goes once
 // through for each adapter that its tokens have, and rows of other adapters are dropped, not multiplied by zero: what is not a number in
-// one request's adapter stays there.
+// one request's adapter stays there. 2011 tokens of five requests and some without, 28672 x 4096, rank 64: 106 us, 22 of them the first product;
+// the second moves 250 MB in 84 us (3 TB/s): a third of that is the start of its CTAs (adapters, z in two parts, the first copies, 6 us each of five
+// waves), in between 64 rows x 256 bytes a tile are on their way at a time.
 #pragma once
 #include "common.cuh"
 
