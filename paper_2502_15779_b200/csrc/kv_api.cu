@@ -88,18 +88,20 @@ int attn_prompt(const rcp::AttnParams& p, cudaStream_t st) {
 }
 
 template <int STEPS>
-int lora_up(rcp::LoraParams p, int tiles, cudaStream_t st) {
+int lora_many(rcp::LoraParams p, int tiles, cudaStream_t st) {
   using L = rcp::UpLayout<STEPS>;
   static std::mutex mu;
-  static bool done[kMaxDevices] = {};
-  RCP_CUDA(set_max_smem(rcp::lora_up_kernel<STEPS>, L::bytes, mu, done));
+  static bool down_done[kMaxDevices] = {}, up_done[kMaxDevices] = {};
+  RCP_CUDA(set_max_smem(rcp::lora_down_kernel<STEPS>, (int)rcp::lora_down_smem(16 * STEPS), mu, down_done));
+  RCP_CUDA(set_max_smem(rcp::lora_up_kernel<STEPS>, L::bytes, mu, up_done));
+  RCP_CUDA(launch_clustered(rcp::lora_down_kernel<STEPS>, dim3(tiles * p.parts), dim3(rcp::kLoraThreads), rcp::lora_down_smem(p.rank), p.parts, st, p));
   // Column tiles of a CTA: few waves of CTAs, and short ones, because tiles in which tokens of two requests meet take twice as long (2011 tokens of
   // six requests, 28672 columns, us a call: 3 tiles a CTA 113, 5 (the choice) 106, 8 105, 13 116, one wave of 25 tiles 135).
   const int cols = (p.N + rcp::kUpCols - 1) / rcp::kUpCols, at_once = sm_count() * std::min<int>(3, 232448 / (L::bytes + 2048));
   double least = 0;
   for (int n = 1; n <= std::min(cols, 16); n++) {
     const int64_t ctas = (int64_t)((cols + n - 1) / n) * tiles;
-    const double cost = (double)((ctas + at_once - 1) / at_once + 1) * (n + 1.5);   // (a CTA's beginning is one tile and a half)
+    const double cost = (double)((ctas + at_once - 1) / at_once + 1) * (n + 0.7);   // (a CTA's beginning is most of a tile)
     if (n == 1 || cost < least) { least = cost; p.up_tiles = n; }
   }
   RCP_CUDA(launch_overlapped(rcp::lora_up_kernel<STEPS>, dim3((cols + p.up_tiles - 1) / p.up_tiles, tiles), dim3(rcp::kLoraThreads), L::bytes, st, p));
@@ -215,7 +217,7 @@ int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads,
 
 size_t rcp_lora_workspace_bytes(int M, int rank) {
   if (M < 1 || M > 65535 || rank < 8 || rank > RCP_LORA_MAX_RANK || rank % 8) return 0;
-  return (size_t)M * rank * sizeof(float);
+  return (size_t)((M + rcp::kLoraTile - 1) / rcp::kLoraTile) * rcp::lora_record_bytes(rank);
 }
 
 int rcp_lora_add(const void* x_f16, int64_t x_stride, const void* a_f16, const void* b_f16, const int32_t* adapter, const float* scaling,
@@ -229,7 +231,7 @@ int rcp_lora_add(const void* x_f16, int64_t x_stride, const void* a_f16, const v
       ((reinterpret_cast<uintptr_t>(base_f16) | reinterpret_cast<uintptr_t>(y_f16)) & 1u))
     return RCP_ERR_ALIGN;
   rcp::LoraParams p{static_cast<const __half*>(x_f16), x_stride, static_cast<const __half*>(a_f16), static_cast<const __half*>(b_f16), adapter,
-                    scaling, static_cast<const __half*>(base_f16), static_cast<__half*>(y_f16), static_cast<float*>(workspace), M, N, K, rank, adapters,
+                    scaling, static_cast<const __half*>(base_f16), static_cast<__half*>(y_f16), static_cast<uint8_t*>(workspace), M, N, K, rank, adapters,
                     1, N % 8 == 0 && aligned16(base_f16) && aligned16(y_f16), 1};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (M <= rcp::kLoraFew) {
@@ -240,19 +242,15 @@ int rcp_lora_add(const void* x_f16, int64_t x_stride, const void* a_f16, const v
   const int tiles = (M + rcp::kLoraTile - 1) / rcp::kLoraTile;
   p.parts = 8;
   while (p.parts > 1 && (tiles * p.parts > 2 * sm_count() || p.parts > K / 64)) p.parts /= 2;
-  static std::mutex mu;
-  static bool done[kMaxDevices] = {};
-  RCP_CUDA(set_max_smem(rcp::lora_down_kernel, (int)rcp::lora_down_smem(rcp::kLoraMaxRank), mu, done));
-  RCP_CUDA(launch_clustered(rcp::lora_down_kernel, dim3(tiles * p.parts), dim3(rcp::kLoraThreads), rcp::lora_down_smem(rank), p.parts, st, p));
   switch ((rank - 1) / 16) {
-    case 0: return lora_up<1>(p, tiles, st);
-    case 1: return lora_up<2>(p, tiles, st);
-    case 2: return lora_up<3>(p, tiles, st);
-    case 3: return lora_up<4>(p, tiles, st);
-    case 4: return lora_up<5>(p, tiles, st);
-    case 5: return lora_up<6>(p, tiles, st);
-    case 6: return lora_up<7>(p, tiles, st);
-    default: return lora_up<8>(p, tiles, st);
+    case 0: return lora_many<1>(p, tiles, st);
+    case 1: return lora_many<2>(p, tiles, st);
+    case 2: return lora_many<3>(p, tiles, st);
+    case 3: return lora_many<4>(p, tiles, st);
+    case 4: return lora_many<5>(p, tiles, st);
+    case 5: return lora_many<6>(p, tiles, st);
+    case 6: return lora_many<7>(p, tiles, st);
+    default: return lora_many<8>(p, tiles, st);
   }
 }
 

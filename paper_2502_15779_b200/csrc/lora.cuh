@@ -14,6 +14,8 @@
 // the second moves 250 MB in 84 us (3 TB/s): a third of that is the start of its CTAs (adapters, z in two parts, the first copies, 6 us each of five
 // waves), in between 64 rows x 256 bytes a tile are on their way at a time.
 #pragma once
+#include <cstddef>
+
 #include "common.cuh"
 
 namespace rcp {
@@ -26,7 +28,7 @@ struct LoraParams {
   const float* scaling;      // [adapters]
   const __half* base;        // [M][N] or null
   __half* y;                 // [M][N]
-  float* z;                  // [M][rank]
+  uint8_t* z;                // a record of lora_record_bytes() for each tile of tokens
   int M, N, K, rank, adapters;
   int parts;                 // CTAs of a cluster of lora_down_kernel: parts of K
   int wide;                  // rows of base and y start on 16 bytes
@@ -233,11 +235,19 @@ __device__ __forceinline__ void lora_mma_first(float (&c)[4], uint4 a, uint32_t 
 }
 
 constexpr int kLoraTile = 64;   // tokens of a tile
-struct LoraTokens {
-  int adapter[kLoraTile];   // of the tile's tokens, -1: none
+struct alignas(16) LoraTokens {
+  int adapter[kLoraTile];   // of the tile's tokens, -1: none, -2: no such token
   int list[kLoraTile];      // the different ones
   int count;
+  int none;                 // whether there are tokens without one
+  int pad[2];
+  float unit[kLoraTile];    // what a token's z in the record is to be multiplied by, a power of two
 };
+// What lora_down_kernel leaves for lora_up_kernel, a tile: its tokens, then z as the tensor core wants it: [upper, lower parts][16 tokens][step
+// of 16 r] of 512 bytes, a lane's 16 bytes side by side.
+constexpr int kLoraRecordZ = 1024;
+static_assert(sizeof(LoraTokens) <= kLoraRecordZ, "");
+__host__ __device__ inline int lora_record_bytes(int rank) { return kLoraRecordZ + (rank + 15) / 16 * 4096; }
 // Fills s; returns how many adapters there are. By one warp in a few votes (one thread with a loop took 4 us).
 __device__ __forceinline__ int tile_adapters(const LoraParams& p, int m0, LoraTokens& s) {
   const int tid = threadIdx.x;
@@ -246,10 +256,11 @@ __device__ __forceinline__ int tile_adapters(const LoraParams& p, int m0, LoraTo
 #pragma unroll
     for (int h = 0; h < 2; h++) {
       const int m = m0 + 32 * h + tid;
-      i[h] = m < p.M ? p.adapter[m] : -1;
-      if (i[h] < 0 || i[h] >= p.adapters) i[h] = -1;
+      i[h] = m < p.M ? p.adapter[m] : -2;
+      if (m < p.M && (i[h] < 0 || i[h] >= p.adapters)) i[h] = -1;
       s.adapter[32 * h + tid] = i[h];
     }
+    const bool none = __any_sync(0xffffffffu, i[0] == -1 || i[1] == -1);
 #pragma unroll
     for (int h = 0; h < 2; h++) {
       const uint32_t alike = __match_any_sync(0xffffffffu, i[h]);   // every lane has to come here, those without an adapter too
@@ -261,7 +272,7 @@ __device__ __forceinline__ int tile_adapters(const LoraParams& p, int m0, LoraTo
       __syncwarp();
       n += __popc(leads);
     }
-    if (tid == 0) s.count = n;
+    if (tid == 0) { s.count = n; s.none = none; }
   }
   __syncthreads();
   return s.count;
@@ -283,7 +294,9 @@ inline size_t lora_down_smem(int rank) { return (size_t)kDownStages * (kLoraTile
 // ring of asynchronous copies (fragments straight from memory took 31 us for 2011 tokens, 4096 elements, rank 64, bound by the cache's
 // ports: every row is wanted by two or four warps). Odd rows have their 64-byte halves exchanged, which keeps the reads of the fragments free
 // of bank conflicts.
-__global__ void __launch_bounds__(kLoraThreads) lora_down_kernel(const LoraParams p) {
+// STEPS: the rank in steps of 16, rounded up (eight columns a warp has at most STEPS times)
+template <int STEPS>
+__global__ void __launch_bounds__(kLoraThreads, 2) lora_down_kernel(const LoraParams p) {
   extern __shared__ __align__(128) uint8_t lora_shared[];
   __shared__ LoraTokens s;
   asm volatile("griddepcontrol.launch_dependents;");
@@ -292,10 +305,13 @@ __global__ void __launch_bounds__(kLoraThreads) lora_down_kernel(const LoraParam
   const uint32_t part = cluster_rank(), base = (uint32_t)__cvta_generic_to_shared(lora_shared);
   const int m0 = (int)blockIdx.x / p.parts * kLoraTile, R = p.rank;
   const int chunks = p.K / 64, c0 = chunks * (int)part / p.parts, c1 = chunks * ((int)part + 1) / p.parts;
-  const int mt = warp & 3, tiles = R / 8, n0 = warp < 4 ? 0 : tiles / 2, nn = warp < 4 ? tiles / 2 : tiles - tiles / 2;   // at most eight
+  const int mt = warp & 3, tiles = R / 8, n0 = warp < 4 ? 0 : tiles / 2, nn = warp < 4 ? tiles / 2 : tiles - tiles / 2;
   const int stage_bytes = (kLoraTile + R) * 128;
   const int different = tile_adapters(p, m0, s);
-  float acc[8][4];
+  uint8_t* const record = p.z + (long long)(m0 / kLoraTile) * lora_record_bytes(R);
+  if (part == 0)
+    for (int v = tid; v < (int)(offsetof(LoraTokens, unit) / 16); v += kLoraThreads) reinterpret_cast<uint4*>(record)[v] = reinterpret_cast<const uint4*>(&s)[v];
+  float acc[STEPS][4];
   for (int e = 0; e < different; e++) {
     const int i = s.list[e];
     // this thread's copies: 16 bytes of every 32nd row, two of tokens, up to four of the adapter
@@ -311,7 +327,7 @@ __global__ void __launch_bounds__(kLoraThreads) lora_down_kernel(const LoraParam
 #pragma unroll
         for (int k = 0; k < 2; k++) { lora_copy16(dst + 32 * 128 * k, from_x[k]); from_x[k] += 64; }
 #pragma unroll
-        for (int k = 0; k < 4; k++)
+        for (int k = 0; k < (STEPS + 1) / 2; k++)
           if (copy_row + 32 * k < R) lora_copy16(dst + (kLoraTile + 32 * k) * 128, from_a + (long long)32 * k * p.K);
         from_a += 64;
         asked++;
@@ -320,7 +336,7 @@ __global__ void __launch_bounds__(kLoraThreads) lora_down_kernel(const LoraParam
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
 #pragma unroll
-    for (int n = 0; n < 8; n++)
+    for (int n = 0; n < STEPS; n++)
 #pragma unroll
       for (int k = 0; k < 4; k++) acc[n][k] = 0.f;
 #pragma unroll
@@ -337,8 +353,8 @@ __global__ void __launch_bounds__(kLoraThreads) lora_down_kernel(const LoraParam
         const uint32_t at = (uint32_t)(((4 * q + j) ^ ((g & 1) << 2)) << 4);
         const uint4 u = lora_lds(xs + (mt * 16 + g) * 128 + at), v = lora_lds(xs + (mt * 16 + 8 + g) * 128 + at);
 #pragma unroll
-        for (int n = 0; n < 8; n++)
-          if (n < nn) {
+        for (int n = 0; n < STEPS; n++)
+          if (n < STEPS - 1 || n < nn) {
             const uint4 w = lora_lds(as + ((n0 + n) * 8 + g) * 128 + at);
             lora_mma(acc[n], u.x, v.x, u.y, v.y, w.x, w.y);
             lora_mma(acc[n], u.z, v.z, u.w, v.w, w.z, w.w);
@@ -349,7 +365,7 @@ __global__ void __launch_bounds__(kLoraThreads) lora_down_kernel(const LoraParam
     __syncthreads();
     float* const out = reinterpret_cast<float*>(lora_shared);   // [tokens][rank]: no more than the ring
 #pragma unroll
-    for (int n = 0; n < 8; n++)
+    for (int n = 0; n < STEPS; n++)
       if (n < nn)
 #pragma unroll
         for (int h = 0; h < 2; h++) {
@@ -358,24 +374,44 @@ __global__ void __launch_bounds__(kLoraThreads) lora_down_kernel(const LoraParam
         }
     // the parts of the cluster's CTAs, each CTA a share of the sums
     cluster_barrier();
-    const int all = kLoraTile * R / 4;
-    for (int v = all * (int)part / p.parts + tid; v < all * ((int)part + 1) / p.parts; v += kLoraThreads) {
-      const int t = 4 * v / R, r = 4 * v - t * R;
+    const int share = kLoraTile / p.parts;
+    const float scaling = p.scaling[i];
+    for (int t = share * (int)part + warp; t < share * ((int)part + 1); t += kLoraWarps) {   // a warp a token, a lane four of its z
       if (s.adapter[t] != i) continue;
-      const uint32_t here = base + (uint32_t)(v * 16);
-      float4 w[8];
+      const int r = 4 * lane;
+      float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (r < R) {
+        const uint32_t here = base + (uint32_t)((t * R + r) * 4);
+        float4 w[8];
 #pragma unroll
-      for (int c = 0; c < 8; c++) {
-        w[c] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (c < p.parts)
-          asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\tld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [a];\n\t}"
-                       : "=f"(w[c].x), "=f"(w[c].y), "=f"(w[c].z), "=f"(w[c].w) : "r"(here), "r"(c) : "memory");
+        for (int c = 0; c < 8; c++) {
+          w[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (c < p.parts)
+            asm volatile("{\n\t.reg .u32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\tld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [a];\n\t}"
+                         : "=f"(w[c].x), "=f"(w[c].y), "=f"(w[c].z), "=f"(w[c].w) : "r"(here), "r"(c) : "memory");
+        }
+#pragma unroll
+        for (int c = 0; c < 8; c++) { z.x += w[c].x; z.y += w[c].y; z.z += w[c].z; z.w += w[c].w; }
+        z.x *= scaling; z.y *= scaling; z.z *= scaling; z.w *= scaling;
       }
-      float4 sum = w[0];
-#pragma unroll
-      for (int c = 1; c < 8; c++) { sum.x += w[c].x; sum.y += w[c].y; sum.z += w[c].z; sum.w += w[c].w; }
-      const float f = p.scaling[i];
-      *reinterpret_cast<float4*>(p.z + (long long)(m0 + t) * R + r) = make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f);
+      // z / 2^exponent in two fp16 numbers, zeroes behind the rank (up to a multiple of 16)
+      const float top = fmaxf(fmaxf(fabsf(z.x), fabsf(z.y)), fmaxf(fabsf(z.z), fabsf(z.w)));
+      const int exponent = min(max((int)(__reduce_max_sync(0xffffffffu, __float_as_uint(top)) >> 23) - 126, -100), 126);   // |z| < 2^exponent
+      const float inv = __int_as_float((127 - exponent) << 23);
+      if (lane == 0) reinterpret_cast<LoraTokens*>(record)->unit[t] = __int_as_float((exponent + 127) << 23);
+      if (r < 16 * STEPS) {
+        z.x *= inv; z.y *= inv; z.z *= inv; z.w *= inv;
+        const __half2 h0 = __floats2half2_rn(z.x, z.y), h1 = __floats2half2_rn(z.z, z.w);
+        const float2 f0 = __half22float2(h0), f1 = __half22float2(h1);
+        const __half2 l0 = __floats2half2_rn(z.x - f0.x, z.y - f0.y), l1 = __floats2half2_rn(z.z - f1.x, z.w - f1.y);
+        // row t % 16 of its 16 tokens, inner elements 4 q .. 4 q + 3 of a step: registers 0 and 2 of lane (t % 8) 4 + q, 1 and 3 for the lower eight rows
+        uint32_t* const to = reinterpret_cast<uint32_t*>(record + kLoraRecordZ + ((t >> 4) * STEPS + (r >> 4)) * 512 + ((t & 7) * 4 + (lane & 3)) * 16) + (t >> 3 & 1);
+        constexpr int lower = kLoraTile / 16 * STEPS * 128;   // in words
+        to[0] = *reinterpret_cast<const uint32_t*>(&h0);
+        to[2] = *reinterpret_cast<const uint32_t*>(&h1);
+        to[lower] = *reinterpret_cast<const uint32_t*>(&l0);
+        to[lower + 2] = *reinterpret_cast<const uint32_t*>(&l1);
+      }
     }
     cluster_barrier();   // nobody overwrites its ring, or ends, while others read from it
   }
@@ -386,8 +422,7 @@ constexpr int kUpCols = 128;   // columns of a tile (32 a warp); a CTA has p.up_
 template <int STEPS>
 struct UpLayout {
   static constexpr int row = STEPS * 16 + 16;                       // halves of a row of b
-  // z as the tensor core wants it: [upper, lower parts][16 tokens][step] of 512 bytes, a lane's 16 bytes of each side by side
-  static constexpr int z = 0, stage0 = 2 * (kLoraTile / 16) * STEPS * 512;
+  static constexpr int z = 0, stage0 = STEPS * 4096;                // z as in the record
   static constexpr int b_bytes = kUpCols * row * 2, base_row = kUpCols * 2 + 16, add_bytes = kLoraTile * base_row;
   static constexpr int add0 = stage0 + 2 * b_bytes, bytes = add0 + 3 * add_bytes;   // (what comes from far away is asked for one tile earlier)
 };
@@ -401,16 +436,19 @@ __global__ void __launch_bounds__(kLoraThreads, STEPS <= 4 ? 2 : 1) lora_up_kern
   using L = UpLayout<STEPS>;
   extern __shared__ __align__(128) uint8_t lora_shared[];
   __shared__ LoraTokens s;
-  __shared__ float s_unit[kLoraTile];
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, j = lane & 3, R = p.rank;
   const uint32_t base = (uint32_t)__cvta_generic_to_shared(lora_shared);
   const int m0 = (int)blockIdx.y * kLoraTile;
-  const int different = tile_adapters(p, m0, s);
+  const uint8_t* const record = p.z + (long long)blockIdx.y * lora_record_bytes(R);
+  if (tid < (int)(sizeof(LoraTokens) / 16)) reinterpret_cast<uint4*>(&s)[tid] = reinterpret_cast<const uint4*>(record)[tid];
+#pragma unroll
+  for (int k = 0; k < STEPS; k++) lora_copy16(base + 16 * (tid + k * kLoraThreads), record + kLoraRecordZ + 16 * (tid + k * kLoraThreads));
+  __syncthreads();
   // passes of a tile: the adapters, and the rows without any if there are some
-  const bool none = __syncthreads_or(tid < kLoraTile && m0 + tid < p.M && s.adapter[tid] < 0);
-  const int passes = different + (none ? 1 : 0), first = (int)blockIdx.x * p.up_tiles, tiles = min(p.up_tiles, (p.N + kUpCols - 1) / kUpCols - first);
+  const int different = s.count, passes = different + (s.none ? 1 : 0);
+  const int first = (int)blockIdx.x * p.up_tiles, tiles = min(p.up_tiles, (p.N + kUpCols - 1) / kUpCols - first);
   // Copies of a thread, 16 bytes each: of b every second piece of one row, of base a piece of every sixteenth row.
   const int b_row = tid >> 1, b_odd = tid & 1, add_row = tid >> 4, add_col = 8 * (tid & 15);
   const uint32_t b_to = base + (uint32_t)(L::stage0 + b_row * L::row * 2 + b_odd * 16);
@@ -420,7 +458,7 @@ __global__ void __launch_bounds__(kLoraThreads, STEPS <= 4 ? 2 : 1) lora_up_kern
 #pragma unroll
   for (int k = 0; k < 4; k++) {
     const int row = add_row + 16 * k;
-    add_adapter[k] = m0 + row < p.M && p.base && p.wide ? s.adapter[row] : -2;
+    add_adapter[k] = p.base && p.wide ? s.adapter[row] : -2;
     add_from[k] = p.base + (long long)(m0 + row) * p.N + first * kUpCols + add_col;
   }
   int b_tile = 0, b_pass = 0, add_tile = 0, add_pass = 0, b_stage = 0, add_stage = 0;
@@ -460,38 +498,6 @@ __global__ void __launch_bounds__(kLoraThreads, STEPS <= 4 ? 2 : 1) lora_up_kern
   load_add();
   load_add();
   asm volatile("cp.async.commit_group;" ::: "memory");
-  // four threads a token: its largest |z|, then z / 2^exponent in two parts, zeroes behind the rank (up to a multiple of 16)
-  {
-    const int t = tid >> 2, q = tid & 3;
-    const bool have = s.adapter[t] >= 0;
-    const float* const z = p.z + (long long)(m0 + t) * R;
-    float top = 0.f;
-    if (have)
-      for (int r = 4 * q; r < R; r += 16) {
-        const float4 v = *reinterpret_cast<const float4*>(z + r);
-        top = fmaxf(fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))), top);
-      }
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const int e = min(max((int)(__float_as_uint(top) >> 23) - 126, -100), 126);   // |z| < 2^e
-    const float inv = __int_as_float((127 - e) << 23);
-    if (q == 0) s_unit[t] = __int_as_float((e + 127) << 23);
-    for (int r = 4 * q; r < STEPS * 16; r += 16) {
-      float4 v = have && r < R ? *reinterpret_cast<const float4*>(z + r) : make_float4(0.f, 0.f, 0.f, 0.f);
-      v.x *= inv; v.y *= inv; v.z *= inv; v.w *= inv;
-      const __half2 h0 = __floats2half2_rn(v.x, v.y), h1 = __floats2half2_rn(v.z, v.w);
-      const float2 f0 = __half22float2(h0), f1 = __half22float2(h1);
-      const __half2 l0 = __floats2half2_rn(v.x - f0.x, v.y - f0.y), l1 = __floats2half2_rn(v.z - f1.x, v.w - f1.y);
-      // row t % 16 of its 16 tokens, inner elements 4 q .. 4 q + 3: registers 0 and 2 of lane (t % 8) 4 + q, 1 and 3 for the lower eight rows
-      uint32_t* const to = reinterpret_cast<uint32_t*>(lora_shared + ((t >> 4) * STEPS + (r >> 4)) * 512 + ((t & 7) * 4 + q) * 16) + (t >> 3 & 1);
-      constexpr int lower = kLoraTile / 16 * STEPS * 128;   // in words
-      to[0] = *reinterpret_cast<const uint32_t*>(&h0);
-      to[2] = *reinterpret_cast<const uint32_t*>(&h1);
-      to[lower] = *reinterpret_cast<const uint32_t*>(&l0);
-      to[lower + 2] = *reinterpret_cast<const uint32_t*>(&l1);
-    }
-  }
-  __syncthreads();
   // this thread's four rows: their adapters (-2: no such row), units and places
   const int t0 = (warp >> 2) * 32;
   int adapter[2][2];
@@ -501,8 +507,8 @@ __global__ void __launch_bounds__(kLoraThreads, STEPS <= 4 ? 2 : 1) lora_up_kern
 #pragma unroll
     for (int h = 0; h < 2; h++) {
       const int t = t0 + m * 16 + h * 8 + g;
-      adapter[m][h] = m0 + t < p.M ? s.adapter[t] : -2;
-      unit[m][h] = s_unit[t];
+      adapter[m][h] = s.adapter[t];
+      unit[m][h] = s.unit[t];
     }
   __half* to[2][2];
 #pragma unroll
