@@ -18,7 +18,7 @@
 // bound by shared memory, 48 clocks each instead of 32), the exponentials' unit 1024. 32 heads on 8, prompts of 2000, 1790 and 1190 tokens behind
 // 3000, 2506 and 2154: 340 us, 836 TFLOP/s; 17 % of it is the last wave of CTAs. Steps: tiles of 128 keys with one tile of scores 446 us; with the 128
 // scores of a row in registers at once (spilled) 529; the next scores read between the exponentials 429 (they are waited for a whole chain too
-// early: the place they go to is free only when the weights in it have been multiplied).
+// early: the place they go to is free only when the weights in it have been multiplied); two threads a row, sixteen softmax warps, 381.
 #pragma once
 #include "kv_attention.cuh"
 #include "ptx.cuh"

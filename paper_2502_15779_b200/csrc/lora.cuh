@@ -10,9 +10,11 @@
 // is free as long as both operands share it, so a thread reads 16 (z) or 8 (y) contiguous bytes. z is a sum in fp32; for the second
 // product each token's row is scaled by a power of two and split into two fp16 numbers, 22 bits of it. A tile goes once
 // through for each adapter that its tokens have, and rows of other adapters are dropped, not multiplied by zero: what is not a number in
-// one request's adapter stays there. 2011 tokens of five requests and some without, 28672 x 4096, rank 64: 106 us, 22 of them the first product;
-// the second moves 250 MB in 84 us (3 TB/s): a third of that is the start of its CTAs (adapters, z in two parts, the first copies, 6 us each of five
-// waves), in between 64 rows x 256 bytes a tile are on their way at a time.
+// one request's adapter stays there. 2011 tokens of five requests and some without, 28672 x 4096, rank 64: 93 us, some 16 of them the first
+// product; the second moves 250 MB in 77 us (3.2 TB/s). Bound by what is on its way at a time (64 rows x 256 bytes a tile, two tiles ahead, two CTAs an
+// SM) and by the two barriers of a pass: without products 91 us. Steps: fragments and base straight from memory 113 us; operands through shared memory
+// 106; z in two parts and in the tensor core's order made by the first kernel, not by every CTA of the second, and the first one's columns known to the
+// compiler 93.
 #pragma once
 #include <cstddef>
 
@@ -428,8 +430,7 @@ struct UpLayout {
 };
 // y of kLoraTile tokens x p.up_tiles * kUpCols columns; a warp has half of the tile's tokens and 32 columns. Column c of n-tile n is column
 // 8 (c / 2) + 2 n + c % 2 of the 32, so that a thread's sums of a row are eight columns side by side and meet base and y in 16 bytes.
-// The next tile's rows of b and of base are on their way to shared memory meanwhile (fragments and base straight from memory: 98 us at 2011
-// tokens, 28672 columns, rank 64, bound by the latency of what was in flight).
+// The next tile's rows of b and of base are on their way to shared memory meanwhile.
 // STEPS: the rank in steps of 16, rounded up
 template <int STEPS>
 __global__ void __launch_bounds__(kLoraThreads, STEPS <= 4 ? 2 : 1) lora_up_kernel(const LoraParams p) {
