@@ -96,7 +96,7 @@ int lora_many(rcp::LoraParams p, int tiles, cudaStream_t st) {
   RCP_CUDA(set_max_smem(rcp::lora_up_kernel<STEPS>, L::bytes, mu, up_done));
   RCP_CUDA(launch_clustered(rcp::lora_down_kernel<STEPS>, dim3(tiles * p.parts), dim3(rcp::kLoraThreads), rcp::lora_down_smem(p.rank), p.parts, st, p));
   // Column tiles of a CTA: few waves of CTAs, and short ones, because tiles in which tokens of two requests meet take twice as long (2011 tokens of
-  // six requests, 28672 columns, us a call, when one took 106: 3 tiles a CTA 113, 5 (the choice) 106, 8 105, 13 116, one wave of 25 tiles 135).
+  // six requests, 28672 columns, us a call: 3 to 6 tiles a CTA 93 (5 is the choice), 8 94.5, 13 105; one wave of 25 tiles 135 against 106 a step before).
   const int cols = (p.N + rcp::kUpCols - 1) / rcp::kUpCols, at_once = sm_count() * std::min<int>(3, 232448 / (L::bytes + 2048));
   double least = 0;
   for (int n = 1; n <= std::min(cols, 16); n++) {

@@ -10,11 +10,11 @@
 // is free as long as both operands share it, so a thread reads 16 (z) or 8 (y) contiguous bytes. z is a sum in fp32; for the second
 // product each token's row is scaled by a power of two and split into two fp16 numbers, 22 bits of it. A tile goes once
 // through for each adapter that its tokens have, and rows of other adapters are dropped, not multiplied by zero: what is not a number in
-// one request's adapter stays there. 2011 tokens of five requests and some without, 28672 x 4096, rank 64: 93 us, some 16 of them the first
-// product; the second moves 250 MB in 77 us (3.2 TB/s). Bound by what is on its way at a time (64 rows x 256 bytes a tile, two tiles ahead, two CTAs an
-// SM) and by the two barriers of a pass: without products 91 us. Steps: fragments and base straight from memory 113 us; operands through shared memory
-// 106; z in two parts and in the tensor core's order made by the first kernel, not by every CTA of the second, and the first one's columns known to the
-// compiler 93.
+// one request's adapter stays there. 2011 tokens of five requests and some without, 28672 x 4096, rank 64: 93 us, 15 of them the first
+// product; the second moves 250 MB in 78 us (3.2 TB/s). Bound by instructions (500 a warp and 32 x 32 results; beside products on mma.sync the others go
+// two a clock, which makes 66 us of them): with neither base nor stores it takes 81 us. Steps: fragments and base straight from memory 113 us;
+// operands through shared memory 106; z in two parts and in the tensor core's order made by the first kernel, not by every CTA of the second, and the
+// first one's columns known to the compiler 93.
 #pragma once
 #include <cstddef>
 
