@@ -100,6 +100,11 @@ __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// the same onto sums of zero
+__device__ __forceinline__ void mma16816_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   uint32_t r;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
@@ -417,7 +422,7 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
 #pragma unroll
       for (int t = 0; t < 2; t++) {
         constexpr int CHAINS = NT < 3 ? 2 : 1;   // products of 16 keys add to CHAINS sums in turn: a shorter chain, where registers allow
-        float part[CHAINS][NT][4] = {};
+        float part[CHAINS][NT][4];
 #pragma unroll
         for (int c = 0; c < KSTEPS / 4; c++) {
           uint4 x[2];
@@ -434,7 +439,10 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
             e4m3_halves(w0[k], a0, a2);
             e4m3_halves(w1[k], a1, a3);
 #pragma unroll
-            for (int n = 0; n < NT; n++) mma16816(part[k % CHAINS][n], a0, a1, a2, a3, q[n][4 * c + k][0], q[n][4 * c + k][1]);
+            for (int n = 0; n < NT; n++) {
+              if (c == 0 && k < CHAINS) mma16816_first(part[k][n], a0, a1, a2, a3, q[n][k][0], q[n][k][1]);
+              else mma16816(part[k % CHAINS][n], a0, a1, a2, a3, q[n][4 * c + k][0], q[n][4 * c + k][1]);
+            }
           }
         }
 #pragma unroll
