@@ -68,11 +68,16 @@ int attn_split(const rcp::AttnParams& p, cudaStream_t st) {
   return RCP_OK;
 }
 
-// Rows of a sequence (new tokens x query heads of a key head) up to which the split kernel takes it: two row tiles of it where the prompt
-// kernel's CTAs, one a key head and sequence, fill the GPU without a split along the keys, nearly three otherwise. Measured, split against
-// prompt kernel, us, 8 key heads, 4000 keys: 16 sequences x 32 rows 69 : 72, x 64 rows 91 : 74; 64 x 32 190 : 226, 64 x 64 257 : 216; 4 x 64
-// 36 : 60; 2 x 64 x 30000 keys 78 : 480; 8 x 48 x 8000 61 : 135.
-int attn_few_rows(int seqs, int kv_heads) { return (int64_t)seqs * kv_heads >= 2 * sm_count() / 3 ? 2 * rcp::kAttnMaxRows : 64; }
+// Rows of a sequence (new tokens x query heads of a key head) up to which the split kernel takes it. Its time goes by sequences x key heads x row
+// tiles of 24 x keys, over all SMs; the prompt kernel's by keys, as long as its CTAs (256 rows of a key head) run at once: no split along the keys.
+// Where the table has room for long sequences the two meet at some 8000 rows x key heads x sequences: split against prompt kernel, us, 8 key heads of
+// 128, 8000 keys: one sequence x 800 rows 132 : 143, two x 256 80 : 145, x 512 162 : 147, four x 256 136 : 149, x 512 247 : 148, eight x 64 71 : 134,
+// x 128 140 : 136; 4000 keys: sixteen x 32 69 : 72, x 64 91 : 74, 64 x 32 190 : 226, x 64 257 : 216. Short sequences: the prompt kernel from the second
+// row tile on (300 keys: one x 64 11 : 10, two x 64 19 : 11, x 256 22 : 18, eight x 64 22 : 11, x 256 36 : 19).
+int attn_few_rows(int seqs, int kv_heads, int64_t room) {
+  if (room <= 1024) return rcp::kAttnMaxRows;
+  return (int)std::min<int64_t>(960, std::max<int64_t>(48, 8000 / ((int64_t)seqs * kv_heads)));
+}
 
 template <int DIM>
 int attn_prompt(const rcp::AttnParams& p, cudaStream_t st) {
@@ -203,7 +208,7 @@ int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads,
   p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + rcp::kAttnPartsAt);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   int64_t rows = (int64_t)p.s.max_new * p.group;
-  const int few = attn_few_rows(seqs, kv_heads);
+  const int few = attn_few_rows(seqs, kv_heads, (int64_t)width * page);
   if (rows > few) {
     p.few = seqs > 1 ? few : 0;
     const int rc2 = dim == 64 ? attn_prompt<64>(p, st) : attn_prompt<128>(p, st);

@@ -116,7 +116,8 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return r;
 }
 
-// x / d for x < 2^16 and d <= 1024, with inv = 2^32 / d rounded up (0 for 1): off by less than x / 2^32 < 1 / d before it is cut off
+// x / d for x < 2^16 and d <= 1024, with inv = 2^32 / d rounded up (0 for 1): off by less than x / 2^32 < 1 / d before it is cut off. (Rows
+// of a sequence are 960 at most here, segments 40 row tiles x 1024 key heads.)
 __device__ __forceinline__ int attn_quotient(int x, uint32_t inv) { return inv ? (int)__umulhi((uint32_t)x, inv) : x; }
 
 // A place in the list of tiles: segment `seg` of sequence b (row tile seg / kv_heads, key head seg % kv_heads), tile of its keys.

@@ -193,6 +193,9 @@ ATTENTION = [
     ([127, 128, 1, 2, 256], [0, 0, 31, 32, 1000], 4, 1, 128, 128),
     ([513, 1], [777, 2], 5, 1, 128, 32),
     ([200, 31], [0, 600], 48, 2, 64, 64),
+    ([200], [2500], 32, 8, 128, 64),
+    ([90, 3, 1], [3000, 10, 2000], 16, 2, 64, 32),
+    ([400], [900], 4, 2, 128, 128),
 ]
 
 
