@@ -45,15 +45,16 @@ struct AttnParams {
   __half* out;               // [tokens][heads][dim]
   int32_t* status;           // set when a bounded wait gives up
   int few;                   // sequences with more rows than that are the prompt kernel's, the others the split kernel's (0: one kernel has all)
-  int32_t* arrived;          // [kAttnMaxCtas], zero between calls
+  int32_t* arrived;          // [2][kAttnMaxCtas], zero between calls: of segments, of groups of CTAs
   float* parts;              // [kAttnMaxCtas][2][rows][dim + 2]
 };
 
 constexpr int kAttnMaxCtas = 256, kAttnMaxRows = 24;
 constexpr int kAttnWarps = 8, kAttnTile = 32;
 constexpr int kAttnAlone = 4;   // tiles a warp
+constexpr int kAttnJoin = 16;   // parts that are joined at once
 constexpr float kAttnSlack = 6.f, kAttnLift = 8.f, kAttnNoMax = -1e30f;
-constexpr size_t kAttnArrivedAt = 256, kAttnPartsAt = kAttnArrivedAt + kAttnMaxCtas * sizeof(int32_t);
+constexpr size_t kAttnArrivedAt = 256, kAttnPartsAt = kAttnArrivedAt + 2 * kAttnMaxCtas * sizeof(int32_t);
 constexpr size_t kAttnWorkspaceBytes = kAttnPartsAt + (size_t)kAttnMaxCtas * 2 * kAttnMaxRows * (128 + 2) * sizeof(float);
 
 // tiles in the ring: three, or two where the parts of 24 rows leave no room
@@ -607,7 +608,9 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
     }
   }
   if (!open) return;
-  // The last of the CTAs that have parts of a segment to arrive here joins them.
+  // The last of the CTAs that have parts of a segment to arrive here joins them, in their order. Of more than 2 kAttnJoin parts it joins what the last to
+  // arrive of each kAttnJoin CTAs have joined, at the first one's place: of 148 parts of 24 rows a join alone is 1.8 MB for one SM (one sequence
+  // of 91439 keys, 24 heads on one: 65 us, with groups 29).
   auto owner = [&](long long unit) {
     const long long big = more * (each + 1);
     return (int)(unit < big ? quotient(unit, each + 1) : more + quotient(unit - big, each));
@@ -620,45 +623,53 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
   __threadfence();
   __syncthreads();
   if (warp == 0 && (open >> lane & 1)) {
-    const int n = atomicAdd(p.arrived + first, 1);
-    if (n == final - first) p.arrived[first] = 0;
-    s_joins[open & ((1u << lane) - 1) ? 1 : 0] = n == final - first;
+    const bool grouped = final - first >= 2 * kAttnJoin;
+    const int from = grouped ? (int)blockIdx.x - ((int)blockIdx.x - first) % kAttnJoin : first, count = grouped ? min(kAttnJoin, final - from + 1) : final - first + 1;
+    bool join = true;   // (a group of one has nothing to wait for; its place among the counters may be another segment's)
+    if (count > 1) {
+      int32_t* const counter = p.arrived + (grouped ? kAttnMaxCtas : 0) + from;
+      join = atomicAdd(counter, 1) == count - 1;
+      if (join) *counter = 0;
+    }
+    s_joins[open & ((1u << lane) - 1) ? 1 : 0] = join;
   }
   __syncthreads();
   for (int k = 0; open; k++, open &= open - 1) {
     if (!s_joins[k]) continue;
-    __threadfence();
     const int s0 = __ffs((int)open) - 1;
     const int cta0 = __shfl_sync(0xffffffffu, first, s0), parts = __shfl_sync(0xffffffffu, final, s0) - cta0 + 1;
     const int seg = __shfl_sync(0xffffffffu, piece.seg, s0), t0 = __shfl_sync(0xffffffffu, piece.t0, s0), n = __shfl_sync(0xffffffffu, piece.n, s0);
-    auto part = [&](int k) { return p.parts + ((size_t)(cta0 + k) * 2 + (k == 0)) * PART; };
-    for (int row = warp; row < ROWS; row += kAttnWarps) {
-      __half* const to = attn_row<DIM>(p, t0, n, seg, ROWS, row);
-      if (!to) break;
-      // references and sums of weights a lane a part, 32 parts at a time; the elements of eight parts are asked for at once
-      float top = kAttnNoMax, sum = 0.f, acc[E] = {};
-      for (int k0 = 0; k0 < parts; k0 += 32) {
-        const bool there = k0 + lane < parts;
-        const float* const ref = part(min(k0 + lane, parts - 1)) + ROWS * DIM + row;
-        const float m = there ? __ldcg(ref) : kAttnNoMax, l = there ? __ldcg(ref + ROWS) : 0.f;
-        float mt = fmaxf(top, m);
+    auto part = [&](int cta) { return p.parts + ((size_t)cta * 2 + (cta == cta0)) * PART; };
+    // joins the parts of `count` CTAs from `from` on, every step-th: to the rows, or (into) to the first one's place
+    auto join = [&](int from, int count, int step, bool into) {
+      __threadfence();
+      for (int row = warp; row < ROWS; row += kAttnWarps) {
+        __half* const to = attn_row<DIM>(p, t0, n, seg, ROWS, row);
+        if (!to) break;
+        // kAttnJoin parts at once: all their elements are asked for, and references and sums of weights a lane a part
+        float top = kAttnNoMax, sum = 0.f, acc[E] = {};
+        for (int k0 = 0; k0 < count; k0 += kAttnJoin) {
+          float2 v[kAttnJoin][E / 2];
 #pragma unroll
-        for (int x = 16; x > 0; x >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, x));
-        const float old = exp2f(top - mt), f = there ? exp2f(m - mt) : 0.f;
-        top = mt;
-        sum *= old;
-#pragma unroll
-        for (int k = 0; k < E; k++) acc[k] *= old;
-        for (int k = 0; k < min(32, parts - k0); k += 8) {
-          float2 v[8][E / 2];
-#pragma unroll
-          for (int u = 0; u < 8; u++)
+          for (int u = 0; u < kAttnJoin; u++)
 #pragma unroll
             for (int d = 0; d < E / 2; d++)
-              v[u][d] = k0 + k + u < parts ? __ldcg(reinterpret_cast<const float2*>(part(k0 + k + u) + row * DIM + E * lane) + d) : make_float2(0.f, 0.f);
+              v[u][d] = k0 + u < count ? __ldcg(reinterpret_cast<const float2*>(part(from + (k0 + u) * step) + row * DIM + E * lane) + d)
+                                       : make_float2(0.f, 0.f);
+          const bool there = lane < kAttnJoin && k0 + lane < count;
+          const float* const ref = part(from + (there ? k0 + lane : k0) * step) + ROWS * DIM + row;
+          const float m = there ? __ldcg(ref) : kAttnNoMax, l = there ? __ldcg(ref + ROWS) : 0.f;
+          float mt = fmaxf(top, m);
 #pragma unroll
-          for (int u = 0; u < 8; u++) {
-            const float fu = __shfl_sync(0xffffffffu, f, k + u), lu = __shfl_sync(0xffffffffu, l, k + u);
+          for (int x = 16; x > 0; x >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, x));
+          const float old = exp2f(top - mt), f = there ? exp2f(m - mt) : 0.f;
+          top = mt;
+          sum *= old;
+#pragma unroll
+          for (int d = 0; d < E; d++) acc[d] *= old;
+#pragma unroll
+          for (int u = 0; u < kAttnJoin; u++) {
+            const float fu = __shfl_sync(0xffffffffu, f, u), lu = __shfl_sync(0xffffffffu, l, u);
             sum += lu * fu;
 #pragma unroll
             for (int d = 0; d < E / 2; d++) {
@@ -667,9 +678,35 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
             }
           }
         }
+        if (!into) {
+          attn_store<E>(to + E * lane, acc, sum > 0.f ? 1.f / sum : sum);
+        } else {
+          float* const place = part(from);
+#pragma unroll
+          for (int d = 0; d < E; d += 2) __stcg(reinterpret_cast<float2*>(place + row * DIM + E * lane + d), make_float2(acc[d], acc[d + 1]));
+          if (lane == 0) {
+            __stcg(place + ROWS * DIM + row, top);
+            __stcg(place + ROWS * (DIM + 1) + row, sum);
+          }
+        }
       }
-      attn_store<E>(to + E * lane, acc, sum > 0.f ? 1.f / sum : sum);
+    };
+    if (parts <= 2 * kAttnJoin) {
+      join(cta0, parts, 1, false);
+      continue;
     }
+    const int from = (int)blockIdx.x - ((int)blockIdx.x - cta0) % kAttnJoin, count = min(kAttnJoin, cta0 + parts - from);
+    const int groups = (parts + kAttnJoin - 1) / kAttnJoin;
+    if (count > 1) join(from, count, 1, true);
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) {
+      const bool all = atomicAdd(p.arrived + cta0, 1) == groups - 1;
+      if (all) p.arrived[cta0] = 0;
+      s_joins[2] = all;
+    }
+    __syncthreads();
+    if (s_joins[2]) join(cta0, groups, kAttnJoin, false);
   }
 }
 

@@ -196,6 +196,9 @@ ATTENTION = [
     ([200], [2500], 32, 8, 128, 64),
     ([90, 3, 1], [3000, 10, 2000], 16, 2, 64, 32),
     ([400], [900], 4, 2, 128, 128),
+    ([1], [20000], 24, 1, 128, 64),
+    ([1, 2], [19000, 12345], 8, 1, 64, 128),
+    ([3, 1, 1], [10000, 15000, 11000], 3, 1, 128, 32),
 ]
 
 
