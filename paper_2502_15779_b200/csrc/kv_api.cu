@@ -72,11 +72,13 @@ int attn_split(const rcp::AttnParams& p, cudaStream_t st) {
 // tiles of 24 x keys, over all SMs; the prompt kernel's by keys, as long as its CTAs (256 rows of a key head) run at once: no split along the keys.
 // Where the table has room for long sequences the two meet at some 8000 rows x key heads x sequences: split against prompt kernel, us, 8 key heads of
 // 128, 8000 keys: one sequence x 800 rows 132 : 143, two x 256 80 : 145, x 512 162 : 147, four x 256 136 : 149, x 512 247 : 148, eight x 64 71 : 134,
-// x 128 140 : 136; 4000 keys: sixteen x 32 69 : 72, x 64 91 : 74, 64 x 32 190 : 226, x 64 257 : 216. Short sequences: the prompt kernel from the second
-// row tile on (300 keys: one x 64 11 : 10, two x 64 19 : 11, x 256 22 : 18, eight x 64 22 : 11, x 256 36 : 19).
+// x 128 140 : 136; 4000 keys: sixteen x 32 69 : 72, x 64 91 : 74, 64 x 32 190 : 226, x 64 257 : 216. Short sequences: as many as the split kernel can give
+// a CTA to each row tile and key head (900 keys: one x 256 15.6 : 25.8, four x 64 15.2 : 19.0, x 256, more than that, 35.7 : 28.0; 300 keys: one x 256
+// 11.3 : 15.9, four x 64 11.3 : 11.2, x 256 27.6 : 18.4).
 int attn_few_rows(int seqs, int kv_heads, int64_t room) {
-  if (room <= 1024) return rcp::kAttnMaxRows;
-  return (int)std::min<int64_t>(960, std::max<int64_t>(48, 8000 / ((int64_t)seqs * kv_heads)));
+  const int64_t segments = (int64_t)seqs * kv_heads;
+  if (room <= 1024) return rcp::kAttnMaxRows * (seqs <= 32 ? (int)std::max<int64_t>(1, sm_count() / segments) : 1);
+  return (int)std::max<int64_t>(2 * rcp::kAttnMaxRows, 8000 / segments);
 }
 
 template <int DIM>
@@ -208,8 +210,10 @@ int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads,
   p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + rcp::kAttnPartsAt);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   int64_t rows = (int64_t)p.s.max_new * p.group;
-  const int few = attn_few_rows(seqs, kv_heads, (int64_t)width * page);
-  if (rows > few) {
+  const int64_t room = (int64_t)width * page;
+  if (rows > attn_few_rows(seqs, kv_heads, room)) {
+    // (the prompt kernel runs anyway, and has CTAs free for all that is not as short as single tokens)
+    const int few = room <= 1024 ? rcp::kAttnMaxRows : 2 * rcp::kAttnMaxRows;
     p.few = seqs > 1 ? few : 0;
     const int rc2 = dim == 64 ? attn_prompt<64>(p, st) : attn_prompt<128>(p, st);
     if (rc2 != RCP_OK || seqs == 1) return rc2;

@@ -22,7 +22,7 @@
 //   warps have, and of a segment that goes on in other CTAs the last one to arrive joins the parts, in their order (so results repeat).
 //   Measured (us, GB/s of what has to be read and written): 64 sequences of 8000 keys at most, 32 heads on 8 of 128: 120, 5.9 TB/s; one of
 //   130999 keys, 64 on 8: 53, 5.0; 16 x 4000, 32 on 32: 63, 5.3; five tokens each of 16 x 8000: 58, 3.2 (three columns of rows; the chain of
-//   operations of a tile, some 1000 instructions on two warps a scheduler); one of 777 keys, dim 64: 7.6, of 20: 3.6. A tile takes a warp some 1700 clocks
+//   operations of a tile, some 1000 instructions on two warps a scheduler); one of 777 keys, dim 64: 7.2, of 20: 3.6. A tile takes a warp some 1700 clocks
 //   however few there are: that is what short sequences wait for. 12 or 16 warps a CTA (fewer registers, parts to memory) were slower everywhere (16 x 4000:
 //   70), and so was nearly everywhere a tile's scores made ahead of the weights of the one in front.
 #pragma once
@@ -118,7 +118,7 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 
 // x / d for x < 2^16 and d <= 1024, with inv = 2^32 / d rounded up (0 for 1): off by less than x / 2^32 < 1 / d before it is cut off. (Rows
-// of a sequence are 960 at most here, segments 40 row tiles x 1024 key heads.)
+// of a sequence are 8000 at most here, 48 where there are hundreds of key heads: attn_few_rows.)
 __device__ __forceinline__ int attn_quotient(int x, uint32_t inv) { return inv ? (int)__umulhi((uint32_t)x, inv) : x; }
 
 // A place in the list of tiles: segment `seg` of sequence b (row tile seg / kv_heads, key head seg % kv_heads), tile of its keys.
@@ -187,10 +187,14 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
   auto quotient = [](long long a, long long b) { return (a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b); };
   AttnPlace at{};
   long long in = 0;   // the share's first tile in its sequence
+  // A CTA a segment, whose warps' parts meet in shared memory, where the longest one takes a warp at most kAttnAlone tiles more than its even share would:
+  // parts that meet in memory cost as much (16 sequences of 300 keys, 32 heads on 8 of 128: 6.7 us, of 1900: 16.0 against 19.1).
+  auto whole = [&](int segs, int tiles) {
+    return segs <= (int)gridDim.x && (long long)tiles * gridDim.x - total <= (long long)kAttnAlone * kAttnWarps * gridDim.x;
+  };
   auto share = [&]() {   // of `total`: as many CTAs as have a tile for each of their warps
     ctas = (int)min((long long)gridDim.x, (total + kAttnWarps - 1) / kAttnWarps);
-    // (a short sequence on its own: a CTA a segment, whose warps' parts meet in shared memory, is faster than parts that meet in memory)
-    if (p.s.seqs == 1 && at.tiles <= kAttnAlone * kAttnWarps && at.segs <= (int)gridDim.x) ctas = at.segs;
+    if (p.s.seqs == 1 && whole(at.segs, at.tiles)) ctas = at.segs;
     if ((int)blockIdx.x >= ctas) return false;
     each = quotient(total, ctas);
     more = total - each * ctas;
@@ -199,23 +203,40 @@ __global__ void __launch_bounds__(kAttnWarps * 32, 1) kv_attention_split_kernel(
     w0 = c0 + (c1 - c0) * warp / kAttnWarps;
     return true;
   };
-  if (p.s.seqs <= 32) {
+  if (p.s.seqs == 1) {
+    attn_sequence<ROWS>(p, 0, at);
+    total = (long long)at.segs * at.tiles;
+    if (!share()) return;
+    in = w0;
+  } else if (p.s.seqs <= 32) {
     if (lane < p.s.seqs) attn_sequence<ROWS>(p, lane, at);
     const long long mine = (long long)at.segs * at.tiles;
     long long upto = mine;
+    int segs = at.segs;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const long long o = __shfl_up_sync(0xffffffffu, upto, d);
-      if (lane >= d) upto += o;
+      const int os = __shfl_up_sync(0xffffffffu, segs, d);
+      if (lane >= d) {
+        upto += o;
+        segs += os;
+      }
     }
+    const int all = __shfl_sync(0xffffffffu, segs, 31);
     total = __shfl_sync(0xffffffffu, upto, 31);
-    if (p.s.seqs == 1) {   // (what follows, without the votes)
-      at.segs = __shfl_sync(0xffffffffu, at.segs, 0);
-      at.tiles = __shfl_sync(0xffffffffu, at.tiles, 0);
+    int b;
+    if (whole(all, (int)__reduce_max_sync(0xffffffffu, at.segs ? at.tiles : 0))) {
+      if ((int)blockIdx.x >= all) return;
+      b = __popc(__ballot_sync(0xffffffffu, segs <= (int)blockIdx.x));   // the first sequence that has segments behind this one
+      c0 = __shfl_sync(0xffffffffu, upto - mine + (long long)((int)blockIdx.x - (segs - at.segs)) * at.tiles, b);
+      c1 = c0 + __shfl_sync(0xffffffffu, at.tiles, b);
+      w0 = c0 + (c1 - c0) * warp / kAttnWarps;
+      each = more = 0;   // (no segment goes on elsewhere)
+    } else {
+      if (!share()) return;
+      // the last sequence with no more than w0 tiles in front of it (it has some itself, or there is nothing to do)
+      b = 31 - __clz((int)__ballot_sync(0xffffffffu, lane < p.s.seqs && upto - mine <= w0));
     }
-    if (!share()) return;
-    // the last sequence with no more than w0 tiles in front of it (it has some itself, or there is nothing to do)
-    const int b = 31 - __clz((int)__ballot_sync(0xffffffffu, lane < p.s.seqs && upto - mine <= w0));
     in = w0 - __shfl_sync(0xffffffffu, upto - mine, b);
     at.b = b;
     at.segs = __shfl_sync(0xffffffffu, at.segs, b);

@@ -199,6 +199,9 @@ ATTENTION = [
     ([1], [20000], 24, 1, 128, 64),
     ([1, 2], [19000, 12345], 8, 1, 64, 128),
     ([3, 1, 1], [10000, 15000, 11000], 3, 1, 128, 32),
+    ([9, 0, 30, 1], [300, 0, 40, 900], 12, 3, 128, 64),
+    ([1] * 32, [i * 7 for i in range(32)], 4, 4, 64, 32),
+    ([2] * 18, [1500] * 18, 16, 8, 64, 128),
 ]
 
 
