@@ -98,10 +98,14 @@ template <int STEPS>
 int lora_many(rcp::LoraParams p, int tiles, cudaStream_t st) {
   using L = rcp::UpLayout<STEPS>;
   static std::mutex mu;
-  static bool down_done[kMaxDevices] = {}, up_done[kMaxDevices] = {};
+  static bool down_done[kMaxDevices] = {}, up_done[2][kMaxDevices] = {};
   RCP_CUDA(set_max_smem(rcp::lora_down_kernel<STEPS>, (int)rcp::lora_down_smem(16 * STEPS), mu, down_done));
-  RCP_CUDA(set_max_smem(rcp::lora_up_kernel<STEPS>, L::bytes, mu, up_done));
-  RCP_CUDA(launch_clustered(rcp::lora_down_kernel<STEPS>, dim3(tiles * p.parts), dim3(rcp::kLoraThreads), rcp::lora_down_smem(p.rank), p.parts, st, p));
+  const bool wide = p.N % 8 == 0 && aligned16(p.base) && aligned16(p.y);
+  const auto up = wide ? rcp::lora_up_kernel<STEPS, true> : rcp::lora_up_kernel<STEPS, false>;
+  RCP_CUDA(set_max_smem(up, L::bytes, mu, up_done[wide]));
+  // A tile's adapters one after another, or among several CTAs where there are few (97 tokens of four adapters, 546 x 3008, rank 56: 34 us, 13 so).
+  const int down_splits = std::max(1, std::min(8, 2 * sm_count() / (tiles * p.parts)));
+  RCP_CUDA(launch_clustered(rcp::lora_down_kernel<STEPS>, dim3(tiles * p.parts, down_splits), dim3(rcp::kLoraThreads), rcp::lora_down_smem(p.rank), p.parts, st, p));
   // Column tiles of a CTA: few waves of CTAs, and short ones, because tiles in which tokens of two requests meet take twice as long (2011 tokens of
   // six requests, 28672 columns, us a call: 3 to 6 tiles a CTA 93 (5 is the choice), 8 94.5, 13 105; one wave of 25 tiles 135 against 106 a step before).
   const int cols = (p.N + rcp::kUpCols - 1) / rcp::kUpCols, at_once = sm_count() * std::min<int>(3, 232448 / (L::bytes + 2048));
@@ -111,7 +115,9 @@ int lora_many(rcp::LoraParams p, int tiles, cudaStream_t st) {
     const double cost = (double)((ctas + at_once - 1) / at_once + 1) * (n + 0.7);   // (a CTA's beginning is most of a tile)
     if (n == 1 || cost < least) { least = cost; p.up_tiles = n; }
   }
-  RCP_CUDA(launch_overlapped(rcp::lora_up_kernel<STEPS>, dim3((cols + p.up_tiles - 1) / p.up_tiles, tiles), dim3(rcp::kLoraThreads), L::bytes, st, p));
+  const int ctas = (cols + p.up_tiles - 1) / p.up_tiles;
+  const int up_splits = (int)std::max<int64_t>(1, std::min<int64_t>(8, at_once / ((int64_t)ctas * tiles)));
+  RCP_CUDA(launch_overlapped(up, dim3(ctas, tiles, up_splits), dim3(rcp::kLoraThreads), L::bytes, st, p));
   return RCP_OK;
 }
 
@@ -241,7 +247,7 @@ int rcp_lora_add(const void* x_f16, int64_t x_stride, const void* a_f16, const v
     return RCP_ERR_ALIGN;
   rcp::LoraParams p{static_cast<const __half*>(x_f16), x_stride, static_cast<const __half*>(a_f16), static_cast<const __half*>(b_f16), adapter,
                     scaling, static_cast<const __half*>(base_f16), static_cast<__half*>(y_f16), static_cast<uint8_t*>(workspace), M, N, K, rank, adapters,
-                    1, N % 8 == 0 && aligned16(base_f16) && aligned16(y_f16), 1};
+                    1, 1};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (M <= rcp::kLoraFew) {
     RCP_CUDA(launch_overlapped(rcp::lora_few_kernel, dim3(M * rcp::kLoraCluster), dim3(rcp::kLoraThreads), 0, st, p));

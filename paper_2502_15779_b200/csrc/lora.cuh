@@ -10,11 +10,11 @@
 // is free as long as both operands share it, so a thread reads 16 (z) or 8 (y) contiguous bytes. z is a sum in fp32; for the second
 // product each token's row is scaled by a power of two and split into two fp16 numbers, 22 bits of it. A tile goes once
 // through for each adapter that its tokens have, and rows of other adapters are dropped, not multiplied by zero: what is not a number in
-// one request's adapter stays there. 2011 tokens of five requests and some without, 28672 x 4096, rank 64: 93 us, 15 of them the first
-// product; the second moves 250 MB in 78 us (3.2 TB/s). Bound by instructions (500 a warp and 32 x 32 results; beside products on mma.sync the others go
+// one request's adapter stays there. 2011 tokens of five requests and some without, 28672 x 4096, rank 64: 90 us, 15 of them the first
+// product; the second moves 250 MB in 75 us (3.3 TB/s). Bound by instructions (500 a warp and 32 x 32 results; beside products on mma.sync the others go
 // two a clock, which makes 66 us of them): with neither base nor stores it takes 81 us. Steps: fragments and base straight from memory 113 us;
 // operands through shared memory 106; z in two parts and in the tensor core's order made by the first kernel, not by every CTA of the second, and the
-// first one's columns known to the compiler 93.
+// first one's columns known to the compiler 93; a kernel of their own for rows that do not start on 16 bytes 90.
 #pragma once
 #include <cstddef>
 
@@ -33,7 +33,6 @@ struct LoraParams {
   uint8_t* z;                // a record of lora_record_bytes() for each tile of tokens
   int M, N, K, rank, adapters;
   int parts;                 // CTAs of a cluster of lora_down_kernel: parts of K
-  int wide;                  // rows of base and y start on 16 bytes
   int up_tiles;              // column tiles of a CTA of lora_up_kernel
 };
 
@@ -311,10 +310,10 @@ __global__ void __launch_bounds__(kLoraThreads, 2) lora_down_kernel(const LoraPa
   const int stage_bytes = (kLoraTile + R) * 128;
   const int different = tile_adapters(p, m0, s);
   uint8_t* const record = p.z + (long long)(m0 / kLoraTile) * lora_record_bytes(R);
-  if (part == 0)
+  if (part == 0 && blockIdx.y == 0)
     for (int v = tid; v < (int)(offsetof(LoraTokens, unit) / 16); v += kLoraThreads) reinterpret_cast<uint4*>(record)[v] = reinterpret_cast<const uint4*>(&s)[v];
   float acc[STEPS][4];
-  for (int e = 0; e < different; e++) {
+  for (int e = (int)blockIdx.y; e < different; e += (int)gridDim.y) {
     const int i = s.list[e];
     // this thread's copies: 16 bytes of every 32nd row, two of tokens, up to four of the adapter
     const int copy_row = tid >> 3, copy_to = copy_row * 128 + (((tid & 7) ^ ((copy_row & 1) << 2)) << 4);
@@ -431,8 +430,8 @@ struct UpLayout {
 // y of kLoraTile tokens x p.up_tiles * kUpCols columns; a warp has half of the tile's tokens and 32 columns. Column c of n-tile n is column
 // 8 (c / 2) + 2 n + c % 2 of the 32, so that a thread's sums of a row are eight columns side by side and meet base and y in 16 bytes.
 // The next tile's rows of b and of base are on their way to shared memory meanwhile.
-// STEPS: the rank in steps of 16, rounded up
-template <int STEPS>
+// STEPS: the rank in steps of 16, rounded up; WIDE: rows of base and y start on 16 bytes
+template <int STEPS, bool WIDE>
 __global__ void __launch_bounds__(kLoraThreads, STEPS <= 4 ? 2 : 1) lora_up_kernel(const LoraParams p) {
   using L = UpLayout<STEPS>;
   extern __shared__ __align__(128) uint8_t lora_shared[];
@@ -447,25 +446,29 @@ __global__ void __launch_bounds__(kLoraThreads, STEPS <= 4 ? 2 : 1) lora_up_kern
 #pragma unroll
   for (int k = 0; k < STEPS; k++) lora_copy16(base + 16 * (tid + k * kLoraThreads), record + kLoraRecordZ + 16 * (tid + k * kLoraThreads));
   __syncthreads();
-  // passes of a tile: the adapters, and the rows without any if there are some
-  const int different = s.count, passes = different + (s.none ? 1 : 0);
+  // passes of a tile: the adapters, and the rows without any if there are some; this CTA has every splits-th
+  const int different = s.count, split = (int)blockIdx.z, splits = (int)gridDim.z, passes = (different + (s.none ? 1 : 0) - split + splits - 1) / splits;
   const int first = (int)blockIdx.x * p.up_tiles, tiles = min(p.up_tiles, (p.N + kUpCols - 1) / kUpCols - first);
   // Copies of a thread, 16 bytes each: of b every second piece of one row, of base a piece of every sixteenth row.
   const int b_row = tid >> 1, b_odd = tid & 1, add_row = tid >> 4, add_col = 8 * (tid & 15);
   const uint32_t b_to = base + (uint32_t)(L::stage0 + b_row * L::row * 2 + b_odd * 16);
   const uint32_t add_to = base + (uint32_t)(L::add0 + add_row * L::base_row + add_col * 2);
+  if (passes <= 0) {
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    return;
+  }
   int add_adapter[4];
   const __half* add_from[4];
 #pragma unroll
   for (int k = 0; k < 4; k++) {
     const int row = add_row + 16 * k;
-    add_adapter[k] = p.base && p.wide ? s.adapter[row] : -2;
+    add_adapter[k] = p.base && WIDE ? s.adapter[row] : -2;
     add_from[k] = p.base + (long long)(m0 + row) * p.N + first * kUpCols + add_col;
   }
   int b_tile = 0, b_pass = 0, add_tile = 0, add_pass = 0, b_stage = 0, add_stage = 0;
   auto load_b = [&]() {   // of the next pass
     if (b_tile < tiles) {
-      const int i = b_pass < different ? s.list[b_pass] : -1, n0 = (first + b_tile) * kUpCols;
+      const int e = split + b_pass * splits, i = e < different ? s.list[e] : -1, n0 = (first + b_tile) * kUpCols;
       if (i >= 0 && n0 + b_row < p.N) {
         const __half* const from = p.b + ((long long)i * p.N + n0 + b_row) * R + 8 * b_odd;
 #pragma unroll
@@ -478,7 +481,7 @@ __global__ void __launch_bounds__(kLoraThreads, STEPS <= 4 ? 2 : 1) lora_up_kern
   };
   auto load_add = [&]() {
     if (add_tile < tiles) {
-      const int i = add_pass < different ? s.list[add_pass] : -1;
+      const int e = split + add_pass * splits, i = e < different ? s.list[e] : -1;
       if ((first + add_tile) * kUpCols + add_col < p.N)
 #pragma unroll
         for (int k = 0; k < 4; k++)
@@ -524,7 +527,7 @@ __global__ void __launch_bounds__(kLoraThreads, STEPS <= 4 ? 2 : 1) lora_up_kern
     asm volatile("cp.async.wait_group 1;" ::: "memory");
     __syncthreads();
     const uint8_t *const st = lora_shared + L::stage0 + (k & 1) * L::b_bytes, *const add_st = lora_shared + L::add0 + add_now * L::add_bytes;
-    const int i = pass < different ? s.list[pass] : -1, col = (first + tile) * kUpCols + (warp & 3) * 32 + 8 * j;
+    const int e = split + pass * splits, i = e < different ? s.list[e] : -1, col = (first + tile) * kUpCols + (warp & 3) * 32 + 8 * j;
     bool mine[2][2], any = false;
 #pragma unroll
     for (int m = 0; m < 2; m++)
@@ -565,13 +568,12 @@ __global__ void __launch_bounds__(kLoraThreads, STEPS <= 4 ? 2 : 1) lora_up_kern
           }
         }
       }
+      if constexpr (WIDE) {
 #pragma unroll
-      for (int m = 0; m < 2; m++)
+        for (int m = 0; m < 2; m++)
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-          if (!mine[m][h]) continue;
-          __half* const at = to[m][h] + col;
-          if (p.wide) {
+          for (int h = 0; h < 2; h++) {
+            if (!mine[m][h]) continue;
             const uint4 add = p.base ? *reinterpret_cast<const uint4*>(add_st + base_at + (m * 16 + h * 8) * L::base_row) : make_uint4(0, 0, 0, 0);
             float v[8];
             halves8(add, v);
@@ -582,17 +584,39 @@ __global__ void __launch_bounds__(kLoraThreads, STEPS <= 4 ? 2 : 1) lora_up_kern
               w[n] = *reinterpret_cast<const uint32_t*>(&y);
             }
             // (without an adapter the row as it is, the signs of its zeroes too)
-            *reinterpret_cast<uint4*>(at) = i < 0 ? add : make_uint4(w[0], w[1], w[2], w[3]);
-          } else {
-            const __half* const add = p.base ? p.base + (at - p.y) : nullptr;
-#pragma unroll
-            for (int x = 0; x < 8; x++)
-              if (col + x < p.N) {
-                const float v = add ? __half2float(add[x]) : 0.f;
-                at[x] = __float2half_rn(i < 0 ? v : fmaf(acc[m][x >> 1][2 * h + (x & 1)], unit[m][h], v));
-              }
+            *reinterpret_cast<uint4*>(to[m][h] + col) = i < 0 ? add : make_uint4(w[0], w[1], w[2], w[3]);
           }
+      } else {
+        // Rows that do not start on 16 bytes: the sums through shared memory (where base would be), so that a warp has 32 columns of one row at a time
+        // (1743 tokens, 21607 columns, rank 56: 234 us with each thread's own eight columns, two bytes a time; 133 so).
+        constexpr int pitch = 36;
+        static_assert(kLoraWarps * 32 * pitch * 4 <= 3 * L::add_bytes, "");
+        float* const sums = reinterpret_cast<float*>(lora_shared + L::add0) + warp * 32 * pitch;
+        if (i >= 0) {
+#pragma unroll
+          for (int m = 0; m < 2; m++)
+#pragma unroll
+            for (int h = 0; h < 2; h++)
+#pragma unroll
+              for (int n = 0; n < 4; n += 2)
+                *reinterpret_cast<float4*>(sums + (m * 16 + h * 8 + g) * pitch + 8 * j + 2 * n) =
+                    make_float4(acc[m][n][2 * h], acc[m][n][2 * h + 1], acc[m][n + 1][2 * h], acc[m][n + 1][2 * h + 1]);
         }
+        __syncwarp();
+        const int c = col - 8 * j + lane;
+        const long long at = (long long)(m0 + t0) * p.N + c;
+        for (int r0 = 0; r0 < 32; r0 += 16) {
+          __half add[16];
+#pragma unroll
+          for (int r = 0; r < 16; r++)
+            add[r] = p.base && c < p.N && s.adapter[t0 + r0 + r] == i ? p.base[at + (long long)(r0 + r) * p.N] : __float2half_rn(0.f);
+#pragma unroll
+          for (int r = 0; r < 16; r++)
+            if (c < p.N && s.adapter[t0 + r0 + r] == i)
+              p.y[at + (long long)(r0 + r) * p.N] =
+                  i < 0 ? add[r] : __float2half_rn(fmaf(sums[(r0 + r) * pitch + lane], s.unit[t0 + r0 + r], __half2float(add[r])));
+        }
+      }
     }
     __syncthreads();
     load_b();
