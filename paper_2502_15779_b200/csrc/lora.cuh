@@ -12,7 +12,7 @@
 // through for each adapter that its tokens have, and rows of other adapters are dropped, not multiplied by zero: what is not a number in
 // one request's adapter stays there. 2011 tokens of five requests and some without, 28672 x 4096, rank 64: 90 us, 15 of them the first
 // product; the second moves 250 MB in 75 us (3.3 TB/s). Bound by instructions (500 a warp and 32 x 32 results; beside products on mma.sync the others go
-// two a clock, which makes 66 us of them): with neither base nor stores it takes 81 us. Steps: fragments and base straight from memory 113 us;
+// two a clock, which makes 66 us of them): with neither base nor stores it took 81 us of 93. Steps: fragments and base straight from memory 113 us;
 // operands through shared memory 106; z in two parts and in the tensor core's order made by the first kernel, not by every CTA of the second, and the
 // first one's columns known to the compiler 93; a kernel of their own for rows that do not start on 16 bytes 90.
 #pragma once
