@@ -35,7 +35,8 @@ def check(got, want, tol):
 
 SHAPES = [(1, 64, 64, 8, 1), (1, 10240, 8192, 16, 8), (1, 1, 128, 8, 3), (2, 33, 192, 24, 2), (3, 5003, 2624, 8, 2), (7, 300, 64, 128, 5),
           (16, 6144, 4096, 32, 48), (16, 999, 14336, 16, 1), (17, 130, 320, 40, 4), (31, 4097, 1088, 64, 3), (33, 64, 65536, 8, 2),
-          (64, 513, 512, 16, 64), (65, 257, 1024, 128, 2), (100, 2048, 2048, 16, 3), (300, 1025, 704, 48, 7), (1000, 129, 256, 72, 2)]
+          (64, 513, 512, 16, 64), (65, 257, 1024, 128, 2), (100, 2048, 2048, 16, 3), (300, 1025, 704, 48, 7), (1000, 129, 256, 72, 2), (97, 546, 2944, 56, 4),
+          (134, 704, 2880, 24, 9), (1100, 2057, 640, 112, 3)]
 
 
 @pytest.mark.parametrize("M,N,K,rank,adapters", SHAPES)
