@@ -479,8 +479,8 @@ int rcp_kv_append(const void* q_f16, int64_t q_stride, const void* k_f16, int64_
  *              results of that call are then invalid, and so are those of later calls until the buffer is zero-filled again.
  * Nothing behind a sequence's length is read: slots that were never written may hold anything.
  * Scores, maxima and sums in fp32; weights are rounded to fp16 for the product with the values, sums stay in fp32. In the kernel
- * for many rows values go through fp16 relative to the largest scale of their 64 positions: exact within 2^11 of it, nothing
- * is left at 2^20.
+ * for many rows values go through fp16 relative to the largest scale of their 64 positions: exact within 2^22 of it, nothing
+ * is left at 2^32 (blocks of 64 and 128 tokens have one scale there).
  * Asynchronous on `stream`; allocates nothing.
  */
 size_t rcp_kv_attention_workspace_bytes(void);

@@ -9,10 +9,11 @@
 // waits for the other's softmax; eight for the softmax, one thread a row. The next tile's scores are made while the softmax works on these.
 // Softmax as in kv_attention.cuh: a row's reference moves only when a score is more than kAttnSlack above it, the sums in tensor memory
 // are rescaled then. (The sum of the weights is of fp32 ones here: tensor memory has no column left for it.) The scales of the values' blocks
-// are folded into the fp16 values relative to a power of two, the unit of the sums, which stays while a tile's largest exponent is within
-// -11 .. 7 of it (fp16 then holds that block's codes exactly) and moves to four above it otherwise; converters and softmax warps follow the same rule on
-// the same scales, so nothing has to be handed over. (A block whose scale is more than 2^11 below that of another one in the same 64 keys loses
-// low bits of its smallest codes, one 2^20 below all of them.)
+// are folded into the fp16 values relative to a power of two, the unit of the sums, which stays while the exponents of a tile's one or two blocks are
+// within -15 .. 7 of it (fp16 holds codes of 2^-9 .. 448 exactly there) and otherwise moves to four above the larger one, less where the smaller one
+// would be out of that range; converters and softmax warps follow the same rule on the same scales, so nothing has to be handed over. (Of two blocks
+// in the same 64 keys, which only pages of 32 have, one whose scale is more than 2^22 below the other's loses low bits of its smallest codes, one 2^32
+// below all of them.)
 // Bound by the softmax warps' chain of a tile: of 2250 clocks factors and masks take 380, the wait for the scores 195, reading them 87, their
 // maximum 470, exponentials, sums and fp16 1090; the tensor pipe is at work 1280 of them (64 keys of both row tiles; the scores' products are
 // bound by shared memory, 48 clocks each instead of 32), the exponentials' unit 1024. 32 heads on 8, prompts of 2000, 1790 and 1190 tokens behind
@@ -102,7 +103,9 @@ struct PromptBlocks {
   int page, next_page;                // -1: none
   float ks, next_ks;
   int ve, next_ve;                    // exponent of the values' scale
-  int unit;                           // exponent of the unit of the sums; INT_MIN in front of the first tile
+  bool calm;                          // these 32 units' exponents are all in the range in which the unit of the sums stays
+  int unit;                           // exponent of the unit of the sums; kNoUnit in front of the first tile
+  static constexpr int kNone = -1000, kNoUnit = 1000;   // of a block that is not there
 
   __device__ __forceinline__ int find(int at) const {   // page of keys 32 at ..
     if (at * 32 >= end) return -1;
@@ -111,25 +114,31 @@ struct PromptBlocks {
   }
   __device__ __forceinline__ void scales(int pg, float& k, int& v) const {
     k = pg >= 0 ? k_scale[(long long)pg * kv_heads + kv] : 1.f;
-    v = pg >= 0 ? kv_stored_exponent(v_scale[(long long)pg * kv_heads + kv]) : INT_MIN;
+    v = pg >= 0 ? kv_stored_exponent(v_scale[(long long)pg * kv_heads + kv]) : kNone;
   }
   __device__ __forceinline__ void start() {
     next_page = find(lane);
     scales(next_page, next_ks, next_ve);
-    unit = INT_MIN;
+    unit = kNoUnit;
+    calm = false;
   }
+  __device__ __forceinline__ bool in_range(int e) const { return e - unit <= 7 && e - unit >= -15; }
   // to be called for every tile in turn; returns by how many powers of two the sums' unit grows with it (0 as a rule)
   __device__ __forceinline__ int step(int tile) {
     if ((tile & 15) == 0) {
       page = next_page; ks = next_ks; ve = next_ve;
+      calm = __all_sync(0xffffffffu, ve == kNone || in_range(ve));
       next_page = find((tile + 16) * 2 + lane);
     }
     if ((tile & 15) == 8) scales(next_page, next_ks, next_ve);
+    if (calm) return 0;
     const int at = (tile & 15) * 2, a = __shfl_sync(0xffffffffu, ve, at), b = __shfl_sync(0xffffffffu, ve, at + 1), top = max(a, b);
-    if (top == INT_MIN) return 0;                       // no keys in this tile
-    if (unit != INT_MIN && top - unit <= 7 && top - unit >= -11) return 0;
-    const int grow = unit == INT_MIN ? 0 : top + 4 - unit;
-    unit = top + 4;
+    if (top == kNone) return 0;                         // no keys in this tile
+    const int low = min(a, b) == kNone ? top : min(a, b);
+    if (in_range(top) && in_range(low)) return 0;
+    const int now = max(min(top + 4, low + 15), top - 7), grow = unit == kNoUnit ? 0 : now - unit;
+    unit = now;
+    calm = __all_sync(0xffffffffu, ve == kNone || in_range(ve));
     return grow;
   }
 };

@@ -484,3 +484,34 @@ def test_cache_beyond_four_gibibytes():
         a = rcp.rcp_kv_attention(q, cache, *tensors(starts, lengths, table))
         b = rcp.rcp_kv_attention(q, small, *tensors(starts, lengths, near))
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dim,kv_heads", [(64, 2), (128, 8)])
+@pytest.mark.parametrize("low", [-11, -12, -14, -20, -22])
+def test_prompt_values_of_unlike_blocks_side_by_side(dim, kv_heads, low):
+    """Pages of 32, two of them in the prompt kernel's 64 keys, whose values' scales differ by 2^4 to 2^15 behind blocks of larger ones; queries look at
+    keys of the small blocks alone, whose values have to come out as exactly as if the large ones were not there."""
+    page, heads, length = 32, 4 * kv_heads, 1200
+    new = 8000 // kv_heads // 4 + 40                                   # more rows than the kernel of few rows takes
+    cache = random_cache(40, kv_heads, page, dim, seed=101, lo=-7, hi=-7)
+    table = make_table([length], page, 40, seed=102)
+    ids = table[0].long().to(DEV)
+    cache.v_scale[ids] = 2.0 ** 8                                      # positions 0 .. 63
+    cache.v_scale[ids[2::2]] = 2.0 ** (8 - 7)                          # from 64 on: the largest of 64 positions
+    cache.v_scale[ids[3::2]] = 2.0 ** (8 + low)                        # and the other block of them
+    value = (torch.arange(dim, device=DEV) % 126 + 1).to(torch.uint8)  # all positive codes, the same row for every token of a small block
+    cache.v.view(torch.uint8)[ids[3::2]] = value
+    key = torch.zeros(dim, device=DEV)
+    key[0] = 448.0
+    cache.k.view(torch.uint8).fill_(0)
+    cache.k[ids[3::2]] = key.to(torch.float8_e4m3fn)                   # a score of 61 and more against zero: the others weigh 2^-88 at most
+    q = torch.zeros(new, heads, dim, dtype=torch.float16, device=DEV)
+    q[:, :, 0] = 200.0
+    want, _ = ref.attention(q, cache, [0, new], [length], table, dim ** -0.5)
+    exact = value.view(torch.float8_e4m3fn).double() * 2.0 ** (8 + low)
+    # the other keys: fewer than 2^11 of magnitude 448 2^8 < 2^17 at 2^-88 of the weight
+    assert bool(((want - exact).abs() <= 2.0 ** -60).all())
+    got = rcp.rcp_kv_attention(q, cache, *tensors([0, new], [length], table))
+    off = (got.double() - want).abs()
+    # weights alike and a power of two: exact; sums of fewer than 2^10 terms in fp32 2^-13; the result to fp16
+    assert bool((off <= (2.0 ** -11 + 2.0 ** -13) * want.abs() + 1.01 * 2.0 ** -25).all()), float((off / want.abs()).max())
