@@ -492,7 +492,9 @@ int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads,
 /*
  * Low-rank adapters of many requests at once, beside a projection that they share (rcp_linear_w2a4 and the others here, or any
  * other): token m uses adapter i = adapter[m],
- *   y[m][n] = fp16( base[m][n] + scaling[i] * sum_r b[i][n][r] * (sum_k a[i][r][k] * x[m][k]) )       (fp32 arithmetic)
+ *   y[m][n] = fp16( base[m][n] + scaling[i] * sum_r b[i][n][r] * (sum_k a[i][r][k] * x[m][k]) )
+ * in fp32 arithmetic. (For more than 64 tokens the inner sum times scaling goes into the outer one with 22 bits; those below 2^-18 of a token's
+ * largest with fewer, off by 2^-40 of that at most.)
  *   x        fp16 [M][K], rows x_stride elements apart (a multiple of 8, at least K); 16-byte aligned. K % 64 == 0.
  *   a, b     fp16 [adapters][rank][K] and [adapters][N][rank], 16-byte aligned, constants like a layer's weights; rank a
  *            multiple of 8 up to RCP_LORA_MAX_RANK (fill a smaller adapter up with zeros).

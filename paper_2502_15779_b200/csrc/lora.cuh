@@ -8,7 +8,7 @@
 // lora_down_kernel, lora_up_kernel: more tokens, as in prompts, in tiles; bound by x, base and y (with hundreds of tokens an
 // adapter is read from L2). Both products on the tensor cores, fragments straight from memory: the order of the inner index
 // is free as long as both operands share it, so a thread reads 16 (z) or 8 (y) contiguous bytes. z is a sum in fp32; for the second
-// product each token's row is scaled by a power of two and split into two fp16 numbers, 22 bits of it. A tile goes once
+// product each token's row is scaled by a power of two and split into two fp16 numbers: 22 bits of each z down to 2^-18 of the row's largest. A tile goes once
 // through for each adapter that its tokens have, and rows of other adapters are dropped, not multiplied by zero: what is not a number in
 // one request's adapter stays there. 2011 tokens of five requests and some without, 28672 x 4096, rank 64: 90 us, 15 of them the first
 // product; the second moves 250 MB in 75 us (3.3 TB/s). Bound by instructions (500 a warp and 32 x 32 results; beside products on mma.sync the others go
@@ -39,6 +39,9 @@ struct LoraParams {
 constexpr int kLoraThreads = 256, kLoraWarps = kLoraThreads / 32;
 constexpr int kLoraFew = 64, kLoraCluster = 8, kLoraGroup = 8;
 constexpr int kLoraMaxRank = 128;
+// A token's z are scaled to below 2^15, as large as fp16 holds them: the two parts' steps then end at 2^-24 beside a largest of 2^15, so that z down to 2^-18 of the
+// token's largest keep 22 bits, and what is lost of smaller ones is 2^-40 of it.
+constexpr int kLoraRoom = 15;
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -395,9 +398,9 @@ __global__ void __launch_bounds__(kLoraThreads, 2) lora_down_kernel(const LoraPa
         for (int c = 0; c < 8; c++) { z.x += w[c].x; z.y += w[c].y; z.z += w[c].z; z.w += w[c].w; }
         z.x *= scaling; z.y *= scaling; z.z *= scaling; z.w *= scaling;
       }
-      // z / 2^exponent in two fp16 numbers, zeroes behind the rank (up to a multiple of 16)
+      // z / 2^exponent, below 2^15, in two fp16 numbers, zeroes behind the rank (up to a multiple of 16)
       const float top = fmaxf(fmaxf(fabsf(z.x), fabsf(z.y)), fmaxf(fabsf(z.z), fabsf(z.w)));
-      const int exponent = min(max((int)(__reduce_max_sync(0xffffffffu, __float_as_uint(top)) >> 23) - 126, -100), 126);   // |z| < 2^exponent
+      const int exponent = min(max((int)(__reduce_max_sync(0xffffffffu, __float_as_uint(top)) >> 23) - 126 - kLoraRoom, -100), 126);   // |z| < 2^(exponent + kLoraRoom)
       const float inv = __int_as_float((127 - exponent) << 23);
       if (lane == 0) reinterpret_cast<LoraTokens*>(record)->unit[t] = __int_as_float((exponent + 127) << 23);
       if (r < 16 * STEPS) {

@@ -225,3 +225,16 @@ def test_attention_half_of_a_decoder_layer(captured):
         out, tol = ref.attention(q_rot, cache, list(range(B + 1)), at, table, dim ** -0.5)
         check(att, out, tol)
         check(o["y"], *ref.lora(att.view(B, -1), o["a"], o["b"], adapter, scaling, o["plain"]))
+
+
+@pytest.mark.parametrize("M,N", [(64, 200), (65, 200), (130, 201)])
+def test_ranks_of_unlike_size(M, N):
+    """Rows of a whose z differ by 2^15 to 2^24 within a token, b scaled the other way: the small z make up as much of the result as the large ones, whether
+    the tokens are few or many."""
+    K, R = 512, 32
+    x, a, b, adapter, scaling, _ = case(M, N, K, R, 2, seed=35)
+    for r, e in enumerate((0, -15, -8, -24, 0, -20, -12, -18) * 4):
+        a[:, r] = (a[:, r].float() * 2.0 ** (10 + e)).half()
+        b[:, :, r] = (b[:, :, r].float() * 2.0 ** (-14 - e)).half()
+    want, tol = ref.lora(x, a, b, adapter, scaling, None)
+    check(rcp.rcp_lora_add(x, a, b, adapter, scaling), want, tol)
