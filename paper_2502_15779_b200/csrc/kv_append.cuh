@@ -17,8 +17,8 @@
 // whole warp. One sequence 2.3 us, 128 sequences with 64 heads on 8 of 128 4.3 (one CTA of the other kernel a block: 10.4).
 // In both, further CTAs rotate queries: a thread takes eight pairs of a token through several heads, so that the 64 bytes of
 // cosines are read once for all of them.
-// Numbers that are not finite are looked for with the maximum (which keeps NaN); only where there are some the values are cut
-// off one by one.
+// Numbers that are not finite or above kKvCap are looked for with the maximum (which keeps NaN); only where there are some the values
+// are cut off one by one.
 #pragma once
 #include "common.cuh"
 #include "kv_common.cuh"
@@ -99,7 +99,7 @@ __device__ __forceinline__ void load_pairs(const float2* at, float2 (&cs)[8]) {
     cs[2 * i + 1] = make_float2(v.z, v.w);
   }
 }
-// finite, NaN as zero: one bad number does not spoil its block
+// kKvCap at most, NaN as zero: one bad number does not spoil its block
 __device__ __forceinline__ float kv_finite(float x) { return x == x ? fminf(fmaxf(x, -kKvCap), kKvCap) : 0.f; }
 __device__ __forceinline__ uint2 codes8(const float (&x)[8], float inv) {
   uint32_t w[4];
@@ -119,7 +119,7 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t c, float f) {
   return r;
 }
 
-// cuts values that are not finite off; returns the largest magnitude then
+// cuts values that are not finite or too large off; returns the largest magnitude then
 __device__ __forceinline__ float make_finite(float (&x)[8], float (&y)[8], float top) {
 #pragma unroll
   for (int k = 0; k < 8; k++) {
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(THREADS) kv_append_kernel(const AppendParams p
       amax = max_abs(max_abs(amax, x[i]), y[i]);
     }
   }
-  if (!(amax < INFINITY)) {
+  if (!(amax <= kKvCap)) {
     amax = 0.f;
 #pragma unroll
     for (int i = 0; i < UNITS; i++) amax = make_finite(x[i], y[i], amax);
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_one_kernel(const App
   float x[8], y[8];
   unit_values(in, have && at.pair >= 0, p.interleaved, cs, x, y);
   float amax = max_abs(max_abs(0.f, x), y);
-  if (!(amax < INFINITY)) amax = make_finite(x, y, 0.f);
+  if (!(amax <= kKvCap)) amax = make_finite(x, y, 0.f);
   uint32_t top = __float_as_uint(amax);
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));

@@ -515,3 +515,23 @@ def test_prompt_values_of_unlike_blocks_side_by_side(dim, kv_heads, low):
     off = (got.double() - want).abs()
     # weights alike and a power of two: exact; sums of fewer than 2^10 terms in fp32 2^-13; the result to fp16
     assert bool((off <= (2.0 ** -11 + 2.0 ** -13) * want.abs() + 1.01 * 2.0 ** -25).all()), float((off / want.abs()).max())
+
+
+@pytest.mark.parametrize("new,cached,page,dim", [([1, 1], [5, 64], 64, 128), ([1], [0], 32, 64), ([40, 3], [10, 0], 32, 64), ([100], [20], 128, 128)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_append_cuts_off_finite_magnitudes_too(new, cached, page, dim, interleaved):
+    """Cosines and sines that carry a factor (as for longer contexts) make keys above 2^17, all of them finite: stored as 2^17."""
+    lengths = [n + c for n, c in zip(new, cached)]
+    cache = random_cache(10, 2, page, dim, seed=111)
+    table = make_table(lengths, page, 10, seed=112)
+    starts, T = starts_of(new), sum(new)
+    k, v = (rand(T, 2, dim, seed=113 + i).clamp(-1, 1) for i in range(2))
+    k[:, 0] *= 60000.0
+    k[0, 1, 3] = 65504.0
+    rope = 4.0 * ref.rope_table(table.shape[1] * page, dim)
+    want, _ = ref.append(cache, k, v, starts, lengths, table, rope, interleaved)
+    rcp.rcp_kv_append(k, v, cache, *tensors(starts, lengths, table), rope=rope, interleaved=interleaved, max_new=max(new))
+    for name, g, w in zip(cache._fields, cache, want):
+        assert same_bits(g, w), name
+    stored = cache.k.float() * cache.k_scale[..., None, None]
+    assert float(stored.abs().max()) == 2.0 ** 17
