@@ -29,7 +29,7 @@ struct KvSeqs {
 struct KvSeq {
   int t0, n;      // its new tokens are rows t0 .. t0 + n - 1
   int first;      // position of the first of them (negative where a length is below the number of new tokens)
-  int end;        // positions that exist: 0 .. end - 1
+  int end;        // positions that exist: 0 .. end - 1 (tokens beyond max_new have none: nothing is stored for them)
 };
 __device__ __forceinline__ KvSeq kv_seq(const KvSeqs& s, int b) {
   KvSeq r;
@@ -39,7 +39,7 @@ __device__ __forceinline__ KvSeq kv_seq(const KvSeqs& s, int b) {
   // (a length is at most what int holds; below zero it is taken as zero, and no more tokens than that have a position)
   r.n = min(t1 - r.t0, s.max_new);
   r.first = max(len, 0) - (t1 - r.t0);
-  r.end = min(max(len, 0), s.width << s.lg_page);
+  r.end = max(min(r.first + r.n, s.width << s.lg_page), 0);
   return r;
 }
 // Sequence of row t (0 <= t < starts[seqs]): the last one that starts at or in front of it.

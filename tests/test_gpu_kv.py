@@ -535,3 +535,20 @@ def test_append_cuts_off_finite_magnitudes_too(new, cached, page, dim, interleav
         assert same_bits(g, w), name
     stored = cache.k.float() * cache.k_scale[..., None, None]
     assert float(stored.abs().max()) == 2.0 ** 17
+
+
+@pytest.mark.parametrize("new,max_new,length,heads,kv_heads", [(50, 20, 200, 4, 2), (9, 1, 300, 8, 2), (300, 265, 1300, 32, 8), (420, 270, 900, 32, 8)])
+@pytest.mark.parametrize("page", [32, 64])
+def test_slots_of_tokens_beyond_max_new_may_hold_anything(new, max_new, length, heads, kv_heads, page):
+    """Tokens beyond max_new are not stored, so their slots may never have been written: NaN in them reaches no row."""
+    dim = 64
+    pages = -(-length // page) + 1
+    cache = random_cache(pages, kv_heads, page, dim, seed=121)
+    table = make_table([length], page, pages, seed=122)
+    q = rand(new, heads, dim, seed=123)
+    want, tol = ref.attention(q, cache, [0, new], [length], table, dim ** -0.5, max_new=max_new)
+    for i in range(length - new + max_new, length):
+        for t in (cache.k, cache.v):
+            t.view(torch.uint8)[int(table[0, i // page]), :, i % page] = 0x7F
+    out = torch.full(q.shape, math.nan, dtype=torch.float16, device=DEV)
+    check_attention(rcp.rcp_kv_attention(q, cache, *tensors([0, new], [length], table), max_new=max_new, out=out), want, tol)
