@@ -503,7 +503,8 @@ int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads,
  *   base     fp16 [M][N], the projection's output; NULL: zero. May be y (the adapters are added in place).
  *   y        fp16 [M][N]. 1 <= M <= 65535, N >= 1.
  *   workspace  rcp_lora_workspace_bytes(M, rank) bytes, 16-byte aligned, zero-filled once; every call leaves it ready for
- *            the next. Calls that may overlap on the GPU need one each.
+ *            the next. Calls that may overlap on the GPU need one each. One zero-filled buffer, large enough for each, may serve
+ *            rcp_lora_add, rcp_kv_attention and the linear calls in turn, in any order, on one stream.
  * Asynchronous on `stream`; allocates nothing.
  */
 #define RCP_LORA_MAX_RANK 128

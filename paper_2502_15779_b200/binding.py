@@ -412,7 +412,8 @@ def make_kv_workspace(device) -> torch.Tensor:
 
 
 def make_lora_workspace(M: int, rank: int, device) -> torch.Tensor:
-    """Zero-filled scratch for rcp_lora_add."""
+    """Zero-filled scratch for rcp_lora_add; one for each stream that calls it (a buffer as large as the larger of the two
+    may serve rcp_kv_attention on that stream as well)."""
     return torch.zeros(max(16, int(lib().rcp_lora_workspace_bytes(M, rank))), dtype=torch.uint8, device=device)
 
 

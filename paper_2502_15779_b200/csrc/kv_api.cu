@@ -94,6 +94,11 @@ int attn_prompt(const rcp::AttnParams& p, cudaStream_t st) {
   return RCP_OK;
 }
 
+// The records of the adapters' tiles stand behind what attention keeps zero in front of its parts (its status and counters; the linear calls' status is the first
+// word too), so that one workspace may serve all of them in turn.
+constexpr size_t kLoraRecordsAt = rcp::kAttnPartsAt;
+static_assert(kLoraRecordsAt % 16 == 0, "records are read 16 bytes at a time");
+
 template <int STEPS>
 int lora_many(rcp::LoraParams p, int tiles, cudaStream_t st) {
   using L = rcp::UpLayout<STEPS>;
@@ -232,7 +237,7 @@ int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads,
 
 size_t rcp_lora_workspace_bytes(int M, int rank) {
   if (M < 1 || M > 65535 || rank < 8 || rank > RCP_LORA_MAX_RANK || rank % 8) return 0;
-  return (size_t)((M + rcp::kLoraTile - 1) / rcp::kLoraTile) * rcp::lora_record_bytes(rank);
+  return kLoraRecordsAt + (size_t)((M + rcp::kLoraTile - 1) / rcp::kLoraTile) * rcp::lora_record_bytes(rank);
 }
 
 int rcp_lora_add(const void* x_f16, int64_t x_stride, const void* a_f16, const void* b_f16, const int32_t* adapter, const float* scaling,
@@ -246,7 +251,7 @@ int rcp_lora_add(const void* x_f16, int64_t x_stride, const void* a_f16, const v
       ((reinterpret_cast<uintptr_t>(base_f16) | reinterpret_cast<uintptr_t>(y_f16)) & 1u))
     return RCP_ERR_ALIGN;
   rcp::LoraParams p{static_cast<const __half*>(x_f16), x_stride, static_cast<const __half*>(a_f16), static_cast<const __half*>(b_f16), adapter,
-                    scaling, static_cast<const __half*>(base_f16), static_cast<__half*>(y_f16), static_cast<uint8_t*>(workspace), M, N, K, rank, adapters,
+                    scaling, static_cast<const __half*>(base_f16), static_cast<__half*>(y_f16), static_cast<uint8_t*>(workspace) + kLoraRecordsAt, M, N, K, rank, adapters,
                     1, 1};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (M <= rcp::kLoraFew) {

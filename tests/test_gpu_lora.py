@@ -238,3 +238,31 @@ def test_ranks_of_unlike_size(M, N):
         b[:, :, r] = (b[:, :, r].float() * 2.0 ** (-14 - e)).half()
     want, tol = ref.lora(x, a, b, adapter, scaling, None)
     check(rcp.rcp_lora_add(x, a, b, adapter, scaling), want, tol)
+
+
+@pytest.mark.parametrize("M", [64, 65, 300])
+def test_one_workspace_for_adapters_and_attention(M):
+    """One zero-filled buffer, large enough for each, for the calls of a stream in turn: what the adapters leave there is not taken for attention's status
+    or counters, and the other way round."""
+    heads, kv_heads, dim, page = 32, 8, 64, 64
+    x, a, b, adapter, scaling, base = case(M, 300, 512, 32, 5, seed=41)
+    cache = rcp.make_kv_cache(300, kv_heads, dim, page, DEV)
+    cases = []
+    for lengths, new in (([9000], 1), ([1500, 40], 300), ([5000, 700, 3], 1)):
+        lengths = [max(n, new) for n in lengths]
+        need = [-(-n // page) for n in lengths]
+        table = torch.full((len(lengths), max(need)), -1, dtype=torch.int32)
+        for i, n in enumerate(need):
+            table[i, :n] = torch.arange(n) + sum(need[:i])
+        starts = torch.arange(len(lengths) + 1, dtype=torch.int32, device=DEV) * new
+        cases.append((rand(len(lengths) * new, heads, dim, seed=42), cache, starts, torch.tensor(lengths, dtype=torch.int32, device=DEV), table.to(DEV)))
+    ws = torch.zeros(max(rcp.make_kv_workspace(DEV).numel(), rcp.make_lora_workspace(M, 32, DEV).numel()), dtype=torch.uint8, device=DEV)
+    k = rand(9000, kv_heads, dim, seed=43)
+    rcp.rcp_kv_append(k, k, cache, *(torch.tensor(t, dtype=torch.int32, device=DEV) for t in ([0, 9000], [9000], [list(range(141))])))
+    want_y = rcp.rcp_lora_add(x, a, b, adapter, scaling, base=base)
+    wants = [rcp.rcp_kv_attention(*c) for c in cases]
+    for _ in range(3):
+        for c, want in zip(cases, wants):
+            assert torch.equal(rcp.rcp_lora_add(x, a, b, adapter, scaling, base=base, workspace=ws), want_y)
+            assert torch.equal(rcp.rcp_kv_attention(*c, workspace=ws), want)
+    assert not ws[:256].any()
