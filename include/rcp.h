@@ -476,7 +476,8 @@ int rcp_kv_append(const void* q_f16, int64_t q_stride, const void* k_f16, int64_
  *   workspace  rcp_kv_attention_workspace_bytes() bytes, 16-byte aligned, zero-filled once; every call leaves it ready
  *              for the next. Calls that may overlap on the GPU need one each. Its first word receives a non-zero code if one of
  *              the bounded waits of the kernel for many rows gives up (3: softmax, 4: conversion, 5: issue; 0 otherwise): the
- *              results of that call are then invalid, and so are those of later calls until the buffer is zero-filled again.
+ *              rows that this leaves without a result are NaN then, and so are those of that kernel in later calls until the
+ *              buffer is zero-filled again.
  * Nothing behind a sequence's length is read: slots that were never written may hold anything.
  * Scores, maxima and sums in fp32; weights are rounded to fp16 for the product with the values, sums stay in fp32. In the kernel
  * for many rows values go through fp16 relative to the largest scale of their 64 positions: exact within 2^22 of it, nothing
@@ -488,6 +489,18 @@ int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads,
                      const int32_t* starts, const int32_t* lengths, const int32_t* table, int seqs, int width, int max_new,
                      const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale, int pages, int page,
                      void* out_f16, void* workspace, void* stream);
+
+/* Same, with the kernel chosen by the caller (for tests, benchmarks and profiles): RCP_ATTENTION_AUTO, RCP_ATTENTION_SPLIT (all keys shared out over
+ * the GPU; max_new, or tokens where it is not known, times heads / kv_heads up to 60000, and fewer than 65536 tiles of 24 of them times kv_heads, else
+ * RCP_ERR_VARIANT) or RCP_ATTENTION_PROMPT (a CTA for 256 rows of a key head). polls: -1, or after how many polls a wait of the kernel for many rows gives up, up to
+ * 2^18, so that the failure report can be tested: with none every wait gives up at once and all rows are NaN, with one some do. The kernel ends either way. */
+#define RCP_ATTENTION_AUTO 0
+#define RCP_ATTENTION_SPLIT 1
+#define RCP_ATTENTION_PROMPT 2
+int rcp_kv_attention_variant(int variant, int polls, const void* q_f16, int64_t q_stride, int tokens, int heads, int kv_heads, int dim, float sm_scale,
+                             const int32_t* starts, const int32_t* lengths, const int32_t* table, int seqs, int width, int max_new,
+                             const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale, int pages, int page,
+                             void* out_f16, void* workspace, void* stream);
 
 /*
  * Low-rank adapters of many requests at once, beside a projection that they share (rcp_linear_w2a4 and the others here, or any

@@ -22,13 +22,14 @@ LIB_PATH = os.environ.get("RCP_W2A4_LIB") or os.path.join(_HERE, "librcp_w2a4.so
 GEMV_AUTO, GEMV_SIMPLE, GEMV_DP4A, GEMV_MMA, GEMV_MMA_ONLY, GEMV_MMA_STREAM, GEMV_UMMA = 0, 1, 2, 3, 4, 5, 6
 VARIANTS = {"auto": GEMV_AUTO, "simple": GEMV_SIMPLE, "dp4a": GEMV_DP4A, "mma": GEMV_MMA, "mma_only": GEMV_MMA_ONLY,
             "mma_stream": GEMV_MMA_STREAM, "umma": GEMV_UMMA}
+ATTENTION_VARIANTS = {"auto": 0, "split": 1, "prompt": 2}
 
 _lib = None
 _m = None   # the native marshalling module, bound to _lib
 _MARSHAL_PATH = marshal_path()
 _MARSHALLED = ("rcp_quantize_act", "rcp_gemv_w2a4_variant", "rcp_gemv_w2a4_grouped_variant", "rcp_gemv_w2a16_checked",
                "rcp_gemv_w3a4", "rcp_linear_w2a4_checked", "rcp_linear_w2a4_host", "rcp_gemv_workspace_bytes",
-               "rcp_kv_append", "rcp_kv_attention", "rcp_kv_attention_workspace_bytes", "rcp_lora_add", "rcp_lora_workspace_bytes",
+               "rcp_kv_append", "rcp_kv_attention_variant", "rcp_kv_attention_workspace_bytes", "rcp_lora_add", "rcp_lora_workspace_bytes",
                "rcp_header_id")
 
 
@@ -98,6 +99,8 @@ def lib():
         L.rcp_kv_attention_workspace_bytes.argtypes = []
         L.rcp_kv_attention.restype = i
         L.rcp_kv_attention.argtypes = [vp, i64, i, i, i, i, C.c_float, vp, vp, vp, i, i, i, vp, vp, vp, vp, i, i, vp, vp, vp]
+        L.rcp_kv_attention_variant.restype = i
+        L.rcp_kv_attention_variant.argtypes = [i, i] + L.rcp_kv_attention.argtypes
         L.rcp_lora_workspace_bytes.restype = u64
         L.rcp_lora_workspace_bytes.argtypes = [i, i]
         L.rcp_lora_add.restype = i
@@ -430,20 +433,30 @@ def rcp_kv_append(k, v, cache, starts, lengths, block_table, rope=None, interlea
     return q_out if q is not None else None
 
 
-def rcp_kv_attention(q, cache, starts, lengths, block_table, sm_scale=None, max_new=0, out=None, workspace=None):
+def rcp_kv_attention(q, cache, starts, lengths, block_table, sm_scale=None, max_new=0, out=None, workspace=None, variant="auto"):
     """Attention of the new tokens q fp16 [tokens][heads][dim] (rotated; rows any distance apart) over the cache, each over the
     positions up to its own -> out fp16 [tokens][heads][dim]. sm_scale: 1/sqrt(dim) by default. The other arguments as for
-    rcp_kv_append, which has to come first."""
+    rcp_kv_append, which has to come first. A program that calls it often keeps out and workspace (without them each call allocates
+    and zero-fills both) and gives max_new (without it a batch of single tokens is set up for prompts). Where a bounded wait of the
+    kernel for many rows gives up, its rows are NaN, in later calls on the same workspace too: kv_attention_status tells.
+    variant: "split" or "prompt" choose the kernel (tests)."""
     if out is None:
         out = torch.zeros(q.shape, dtype=torch.float16, device=q.device)
     if workspace is None:
         workspace = make_kv_workspace(q.device)
     if sm_scale is None:
         sm_scale = q.shape[-1] ** -0.5
-    st = (_m or _native()).kv_attention(q, *cache, starts, lengths, block_table, sm_scale, max_new, out, workspace)
+    st = (_m or _native()).kv_attention(q, *cache, starts, lengths, block_table, sm_scale, max_new, out, workspace,
+                                    ATTENTION_VARIANTS[variant])
     if st:
         _check("rcp_kv_attention", st)
     return out
+
+
+def kv_attention_status(workspace) -> int:
+    """0, or the code that rcp_kv_attention left in its workspace when a wait gave up (3, 4 or 5; zero-fill it to go on). Waits for the calls in
+    front of it."""
+    return int(workspace[:4].view(torch.int32))
 
 
 def rcp_lora_add(x, a, b, adapter, scaling, base=None, y=None, workspace=None):

@@ -31,7 +31,7 @@ struct Entry {
   decltype(&rcp_linear_w2a4_host) linear_host = nullptr;
   decltype(&rcp_gemv_workspace_bytes) workspace_bytes = nullptr;
   decltype(&rcp_kv_append) kv_append = nullptr;
-  decltype(&rcp_kv_attention) kv_attention = nullptr;
+  decltype(&rcp_kv_attention_variant) kv_attention = nullptr;
   decltype(&rcp_kv_attention_workspace_bytes) kv_workspace_bytes = nullptr;
   decltype(&rcp_lora_add) lora_add = nullptr;
   decltype(&rcp_lora_workspace_bytes) lora_workspace_bytes = nullptr;
@@ -175,7 +175,7 @@ PyObject* bind(PyObject*, PyObject* table) {
       !take("rcp_gemv_w2a4_grouped_variant", g_fn.gemv_grouped) || !take("rcp_gemv_w2a16_checked", g_fn.gemv_w2a16) ||
       !take("rcp_gemv_w3a4", g_fn.gemv_w3a4) || !take("rcp_linear_w2a4_checked", g_fn.linear) ||
       !take("rcp_linear_w2a4_host", g_fn.linear_host) || !take("rcp_gemv_workspace_bytes", g_fn.workspace_bytes) ||
-      !take("rcp_kv_append", g_fn.kv_append) || !take("rcp_kv_attention", g_fn.kv_attention) ||
+      !take("rcp_kv_append", g_fn.kv_append) || !take("rcp_kv_attention_variant", g_fn.kv_attention) ||
       !take("rcp_kv_attention_workspace_bytes", g_fn.kv_workspace_bytes) || !take("rcp_lora_add", g_fn.lora_add) ||
       !take("rcp_lora_workspace_bytes", g_fn.lora_workspace_bytes))
     return nullptr;
@@ -457,15 +457,15 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (q, cache.k, cache.v, cache.k_scale, cache.v_scale, starts, lengths, block_table, sm_scale, max_new, out, workspace)
+// (q, cache.k, cache.v, cache.k_scale, cache.v_scale, starts, lengths, block_table, sm_scale, max_new, out, workspace, variant)
 PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
     Cache c;
     int64_t qs;
-    int max_new;
+    int max_new, variant;
     float sm_scale;
     void *out, *ws;
-    if (!count(n, 12)) return nullptr;
+    if (!count(n, 13) || !integer(a[12], &variant)) return nullptr;
     const at::Tensor* q = rows(a[0], "q", 3, nullptr, &qs);
     if (!q || !cache_of(a + 1, q, &c) || !real(a[8], &sm_scale) || !integer(a[9], &max_new)) return nullptr;
     const int64_t T = q->size(0), heads = q->size(1);
@@ -476,7 +476,7 @@ PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const float *ksc = static_cast<const float*>(c.ks->data_ptr()), *vsc = static_cast<const float*>(c.vs->data_ptr());
     const int32_t *st = ints(c.starts), *ln = ints(c.lengths), *tb = ints(c.table);
     return on_device(*q, [&](void* stream) {
-      return g_fn.kv_attention(qp, qs, (int)T, (int)heads, c.kv_heads, c.dim, sm_scale, st, ln, tb, c.seqs, c.width, max_new, kc, vc, ksc, vsc, c.pages,
+      return g_fn.kv_attention(variant, -1, qp, qs, (int)T, (int)heads, c.kv_heads, c.dim, sm_scale, st, ln, tb, c.seqs, c.width, max_new, kc, vc, ksc, vsc, c.pages,
                                c.page, out, ws, stream);
     });
   });

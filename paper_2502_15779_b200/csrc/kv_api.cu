@@ -193,9 +193,12 @@ int rcp_kv_append(const void* q_f16, int64_t q_stride, const void* k_f16, int64_
 
 size_t rcp_kv_attention_workspace_bytes(void) { return rcp::kAttnWorkspaceBytes; }
 
-int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads, int kv_heads, int dim, float sm_scale, const int32_t* starts,
-                     const int32_t* lengths, const int32_t* table, int seqs, int width, int max_new, const void* k_cache, const void* v_cache,
-                     const float* k_scale, const float* v_scale, int pages, int page, void* out_f16, void* workspace, void* stream) {
+int rcp_kv_attention_variant(int variant, int polls, const void* q_f16, int64_t q_stride, int tokens, int heads, int kv_heads, int dim, float sm_scale,
+                             const int32_t* starts, const int32_t* lengths, const int32_t* table, int seqs, int width, int max_new, const void* k_cache,
+                             const void* v_cache, const float* k_scale, const float* v_scale, int pages, int page, void* out_f16, void* workspace,
+                             void* stream) {
+  if (variant < RCP_ATTENTION_AUTO || variant > RCP_ATTENTION_PROMPT) return RCP_ERR_VARIANT;
+  if (polls < -1 || polls > (int)rcp::kPromptPolls) return RCP_ERR_SHAPE;
   if (!q_f16 || !out_f16) return RCP_ERR_NULL;
   rcp::AttnParams p{};
   const int rc = check_cache(tokens, heads, kv_heads, dim, starts, lengths, table, seqs, width, max_new, k_cache, v_cache, k_scale, v_scale, pages,
@@ -217,12 +220,16 @@ int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads,
   p.k_scale = k_scale; p.v_scale = v_scale;
   p.out = static_cast<__half*>(out_f16);
   p.status = static_cast<int32_t*>(workspace);
+  p.polls = polls >= 0 ? (uint32_t)polls : rcp::kPromptPolls;
   p.arrived = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(workspace) + rcp::kAttnArrivedAt);
   p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + rcp::kAttnPartsAt);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   int64_t rows = (int64_t)p.s.max_new * p.group;
   const int64_t room = (int64_t)width * page;
-  if (rows > attn_few_rows(seqs, kv_heads, room)) {
+  // (attn_quotient: rows and segments of a sequence below 2^16)
+  if (variant == RCP_ATTENTION_SPLIT && (rows > 60000 || (rows + rcp::kAttnMaxRows - 1) / rcp::kAttnMaxRows * kv_heads > 65535)) return RCP_ERR_VARIANT;
+  if (variant == RCP_ATTENTION_PROMPT) return dim == 64 ? attn_prompt<64>(p, st) : attn_prompt<128>(p, st);
+  if (variant == RCP_ATTENTION_AUTO && rows > attn_few_rows(seqs, kv_heads, room)) {
     // (the prompt kernel runs anyway, and has CTAs free for all that is not as short as single tokens)
     const int few = room <= 1024 ? rcp::kAttnMaxRows : 2 * rcp::kAttnMaxRows;
     p.few = seqs > 1 ? few : 0;
@@ -233,6 +240,13 @@ int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads,
   const int nt = rows <= 8 ? 1 : rows <= 16 ? 2 : 3;
   if (dim == 64) return nt == 1 ? attn_split<64, 1>(p, st) : nt == 2 ? attn_split<64, 2>(p, st) : attn_split<64, 3>(p, st);
   return nt == 1 ? attn_split<128, 1>(p, st) : nt == 2 ? attn_split<128, 2>(p, st) : attn_split<128, 3>(p, st);
+}
+
+int rcp_kv_attention(const void* q_f16, int64_t q_stride, int tokens, int heads, int kv_heads, int dim, float sm_scale, const int32_t* starts,
+                     const int32_t* lengths, const int32_t* table, int seqs, int width, int max_new, const void* k_cache, const void* v_cache,
+                     const float* k_scale, const float* v_scale, int pages, int page, void* out_f16, void* workspace, void* stream) {
+  return rcp_kv_attention_variant(RCP_ATTENTION_AUTO, -1, q_f16, q_stride, tokens, heads, kv_heads, dim, sm_scale, starts, lengths, table, seqs, width, max_new,
+                                  k_cache, v_cache, k_scale, v_scale, pages, page, out_f16, workspace, stream);
 }
 
 size_t rcp_lora_workspace_bytes(int M, int rank) {

@@ -28,7 +28,7 @@ namespace rcp {
 
 constexpr int kPromptThreads = 512, kPromptRows = 256, kPromptKeys = 64, kPromptStages = 4;
 
-constexpr uint32_t kPromptPolls = 1u << 18;   // a wait of this kernel is a few microseconds
+constexpr uint32_t kPromptPolls = 1u << 18;   // p.polls as a rule: a wait of this kernel is a few microseconds
 
 template <int DIM>
 struct PromptLayout {
@@ -73,7 +73,6 @@ __device__ __forceinline__ void umma_ts(uint32_t elected, uint32_t d, uint32_t a
                : "memory");
 }
 
-__device__ __forceinline__ bool prompt_wait(uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, kPromptPolls); }
 
 // two fp32 numbers at a time
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
@@ -164,11 +163,19 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
   const KvSeq sq = kv_seq(p.s, lo);
   const int b = lo, tile_row = (cand - (int)((long long)p.s.starts[b] * p.group / kPromptRows) - b) * kPromptRows;
   const int total_rows = sq.n * p.group, rows = min(total_rows - tile_row, kPromptRows);
-  // few rows are the other kernel's (which runs beside this one unless there is but one sequence). Behind a wait that gave up nothing
-  // more is waited for: the results are invalid already.
+  // Few rows are the other kernel's, which is launched behind this one unless there is but one sequence. Behind a wait that gave up nothing
+  // more is waited for: the rows are NaN until the status is cleared.
   const int gave_up = __syncthreads_or(tid == 0 && *reinterpret_cast<volatile int32_t*>(p.status) != 0);
-  if (gave_up || tile_row < 0 || rows <= 0 || total_rows <= p.few) {
+  const bool mine = tile_row >= 0 && rows > 0 && total_rows > p.few;
+  constexpr uint32_t kNoResult = 0x7FFF7FFFu;   // NaN
+  if (gave_up || !mine) {
     asm volatile("griddepcontrol.launch_dependents;");
+    if (mine)
+      for (int x = tid; x < rows * (DIM / 8); x += kPromptThreads) {
+        const int r = tile_row + x / (DIM / 8), i = r / p.group;
+        *reinterpret_cast<uint4*>(p.out + ((long long)(sq.t0 + i) * p.heads + (long long)kv * p.group + (r - i * p.group)) * DIM + x % (DIM / 8) * 8) =
+            make_uint4(kNoResult, kNoResult, kNoResult, kNoResult);
+      }
     return;
   }
   const int last_pos = sq.first + (tile_row + rows - 1) / p.group;
@@ -224,6 +231,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
   blocks.kv = kv; blocks.kv_heads = p.kv_heads; blocks.end = sq.end; blocks.lane = lane;
   constexpr uint32_t kS = 0, kO = 256;   // tensor memory: scores (and weights) of the row tiles, then their sums
   bool ok = true;
+  auto prompt_wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, p.polls); };
 
   if (warp < 8) {
     // ---------------------------------------------------------------- softmax: a thread a row
@@ -315,8 +323,12 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
       }
       if (ok) ok = prompt_wait(drained + 8 * half, 0);
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      __half* const to = p.out + ((long long)(sq.t0 + i) * p.heads + (long long)kv * p.group + (r - i * p.group)) * DIM;
+      if (!ok && have) {
+#pragma unroll
+        for (int d = 0; d < DIM / 8; d++) reinterpret_cast<uint4*>(to)[d] = make_uint4(kNoResult, kNoResult, kNoResult, kNoResult);
+      }
       if (ok) {
-        __half* const to = p.out + ((long long)(sq.t0 + i) * p.heads + (long long)kv * p.group + (r - i * p.group)) * DIM;
         const float f = l > 0.f ? kv_pow2(min(max(blocks.unit, -100), 100)) / l : l;
 #pragma unroll
         for (int d = 0; d < DIM / 32; d++) {
@@ -469,10 +481,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
         umma_commit(elected, o_done + 8 * half);
         umma_commit(elected, v_empty + 8 * stage);
       }
-      // nothing of this warp is at work any more when tensor and shared memory are given back
+      // nothing of this warp is at work any more when tensor and shared memory are given back (waited for with the full limit whatever p.polls is)
       umma_commit(elected, drained + 8 * half);
       __syncwarp();
-      prompt_wait(drained + 8 * half, 0);
+      mbar_wait_warp(drained + 8 * half, 0, kPromptPolls);
     }
   }
   if (!ok && lane == 0) atomicExch(p.status, warp < 8 ? 3 : warp < 12 ? 4 : 5);

@@ -552,3 +552,55 @@ def test_slots_of_tokens_beyond_max_new_may_hold_anything(new, max_new, length, 
             t.view(torch.uint8)[int(table[0, i // page]), :, i % page] = 0x7F
     out = torch.full(q.shape, math.nan, dtype=torch.float16, device=DEV)
     check_attention(rcp.rcp_kv_attention(q, cache, *tensors([0, new], [length], table), max_new=max_new, out=out), want, tol)
+
+
+def attention_with_polls(polls, q, cache, starts, lengths, table, out, workspace, variant="prompt"):
+    """rcp_kv_attention_variant with a limit of its own for the waits"""
+    p = lambda t: t.data_ptr()
+    pages, kv_heads, page, dim = cache.k.shape
+    assert rcp.lib().rcp_kv_attention_variant(
+        rcp.binding.ATTENTION_VARIANTS[variant], polls, p(q), q.stride(0), q.shape[0], q.shape[1], kv_heads, dim, dim ** -0.5, p(starts), p(lengths),
+        p(table), table.shape[0], table.shape[1], 0, p(cache.k), p(cache.v), p(cache.k_scale), p(cache.v_scale), pages, page, p(out), p(workspace),
+        torch.cuda.current_stream().cuda_stream) == 0
+    return out
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attention_that_gave_up_leaves_nan_and_a_status(dim):
+    """Waits with no polls give up at once, with one poll some do: rows are NaN or right, the status says so, the kernel ends and the GPU goes on. The next
+    calls on the workspace give NaN until it is cleared; sequences of the kernel of few rows are answered all the same."""
+    page, heads, kv_heads = 64, 8, 2
+    new, lengths = [300, 2, 40], [5000, 700, 300]
+    pages = sum(-(-n // page) for n in lengths)
+    cache = random_cache(pages, kv_heads, page, dim, seed=131)
+    starts = starts_of(new, 1)
+    args = tensors(starts, lengths, make_table(lengths, page, pages, seed=132))
+    q, ws = rand(sum(new) + 2, heads, dim, seed=133), rcp.make_kv_workspace(DEV)
+    mine = slice(starts[0], starts[-1])
+    want = rcp.rcp_kv_attention(q, cache, *args, workspace=ws, variant="prompt")
+    assert rcp.kv_attention_status(ws) == 0
+    out = attention_with_polls(0, q, cache, *args, torch.zeros_like(want), ws)
+    assert rcp.kv_attention_status(ws) in (3, 4, 5)
+    assert bool(torch.isnan(out[mine]).all()) and not out[:1].any() and not out[-1:].any()
+    # status set: in front of every wait
+    out = rcp.rcp_kv_attention(q, cache, *args, workspace=ws, variant="prompt")
+    assert bool(torch.isnan(out[mine]).all()) and not out[:1].any() and not out[-1:].any() and rcp.kv_attention_status(ws) in (3, 4, 5)
+    # one poll a wait
+    for _ in range(30):
+        ws.zero_()
+        out = attention_with_polls(1, q, cache, *args, torch.zeros_like(want), ws)
+        bad = torch.isnan(out).any(-1)
+        assert torch.equal(out[~bad], want[~bad]) and bool(torch.isnan(out[bad]).all()) and (rcp.kv_attention_status(ws) != 0 or not bool(bad.any()))
+    ws.zero_()
+    assert torch.equal(rcp.rcp_kv_attention(q, cache, *args, workspace=ws, variant="prompt"), want) and rcp.kv_attention_status(ws) == 0
+    # both kernels in one call: rows of a key head up to 24 or 48 are the other kernel's
+    heads, kv_heads, new, lengths = 32, 8, [300, 2], [1500, 1400]
+    cache = random_cache(48, kv_heads, page, dim, seed=134)
+    args = tensors(starts_of(new), lengths, make_table(lengths, page, 48, seed=135))
+    q = rand(302, heads, dim, seed=136)
+    want = rcp.rcp_kv_attention(q, cache, *args, workspace=ws)
+    ws[0] = 3
+    out = rcp.rcp_kv_attention(q, cache, *args, workspace=ws)
+    assert bool(torch.isnan(out[:300]).all()) and torch.equal(out[300:], want[300:])
+    # without a workspace of one's own, too, nothing looks like a result that is none
+    assert torch.equal(rcp.rcp_kv_attention(q, cache, *args), want)

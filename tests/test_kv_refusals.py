@@ -148,3 +148,22 @@ def test_binding_refuses_wrong_shapes_on_the_gpu(L):
             rcp.rcp_lora_add(*bad)
     with pytest.raises(ValueError, match="base"):
         rcp.rcp_lora_add(xx, a, b, adapter, scaling, base=torch.zeros(2, 5, dtype=torch.float16, device=dev))
+
+
+VARIANT = -7
+
+
+@pytest.mark.parametrize("status,change", [
+    (VARIANT, dict(variant=3)), (VARIANT, dict(variant=-1)), (SHAPE, dict(polls=-2)), (SHAPE, dict(polls=(1 << 18) + 1)),
+    # more rows, or more tiles of them, than the split kernel counts
+    (VARIANT, dict(variant=1, tokens=15001, qs=512)), (VARIANT, dict(variant=1, tokens=1 << 20, max_new=15001, qs=512)),
+    (VARIANT, dict(variant=1, tokens=1536, heads=1024, kv_heads=1024, qs=65536)),
+    (NULL, dict(q=None)), (WORKSPACE, dict(workspace=None)), (SHAPE, dict(dim=96))])
+def test_attention_of_a_chosen_kernel_refuses(L, status, change):
+    assert call(L.rcp_kv_attention_variant, dict(variant=0, polls=-1, **ATTENTION), **change) == status
+
+
+def test_binding_refuses_an_unknown_attention_kernel(L):
+    x = torch.zeros(1, 1, 64, dtype=torch.float16)
+    with pytest.raises(KeyError):
+        rcp.rcp_kv_attention(x, rcp.make_kv_cache(2, 1, 64, 32, "cpu"), x, x, x, out=x, workspace=x, variant="best")
