@@ -449,6 +449,10 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void *kc = c.k->data_ptr(), *vc = c.v->data_ptr();
     float *ksc = static_cast<float*>(c.ks->data_ptr()), *vsc = static_cast<float*>(c.vs->data_ptr());
     const int32_t *st = ints(c.starts), *ln = ints(c.lengths), *tb = ints(c.table);
+    if (T == 0) {   // empty tensors have no address; the library looks at none of these then
+      kp = vp = kc;
+      if (q) qp = q_out = kc;
+    }
     const int positions = rope ? (int)rope->size(0) : 0, rot = rope ? 2 * (int)rope->size(1) : 0;
     return on_device(*k, [&](void* stream) {
       return g_fn.kv_append(qp, qs, kp, ks, vp, vs, (int)T, heads, c.kv_heads, c.dim, rp, positions, rot, interleaved, st, ln, tb, c.seqs, c.width,
@@ -473,6 +477,7 @@ PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!buffer(a[10], "out", at::kHalf, *q, q->numel(), &out) || !buffer(a[11], "workspace", kAny, *q, (int64_t)g_fn.kv_workspace_bytes(), &ws))
       return nullptr;
     const void *qp = q->data_ptr(), *kc = c.k->data_ptr(), *vc = c.v->data_ptr();
+    if (T == 0) qp = out = c.k->data_ptr();   // as in kv_append
     const float *ksc = static_cast<const float*>(c.ks->data_ptr()), *vsc = static_cast<const float*>(c.vs->data_ptr());
     const int32_t *st = ints(c.starts), *ln = ints(c.lengths), *tb = ints(c.table);
     return on_device(*q, [&](void* stream) {

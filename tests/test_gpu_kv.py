@@ -604,3 +604,19 @@ def test_attention_that_gave_up_leaves_nan_and_a_status(dim):
     assert bool(torch.isnan(out[:300]).all()) and torch.equal(out[300:], want[300:])
     # without a workspace of one's own, too, nothing looks like a result that is none
     assert torch.equal(rcp.rcp_kv_attention(q, cache, *args), want)
+
+
+def test_calls_without_tokens():
+    """A step in which no sequence has a new token: empty tensors, nothing stored, an empty result."""
+    cache = random_cache(4, 2, 32, 64, seed=141)
+    before = [t.clone() for t in cache]
+    args = tensors([0, 0, 0], [20, 0], torch.tensor([[1], [2]], dtype=torch.int32))
+    row = torch.empty(0, 8, 64, dtype=torch.float16, device=DEV)
+    q, k, v = row[:, :4], row[:, 4:6], row[:, 6:]
+    assert rcp.rcp_kv_append(k, v, cache, *args) is None
+    for q_out in (None, torch.empty(0, 4, 64, dtype=torch.float16, device=DEV)):
+        assert rcp.rcp_kv_append(k, v, cache, *args, rope=ref.rope_table(32, 64), q=q, q_out=q_out).shape == (0, 4, 64)
+    for variant in ("auto", "split", "prompt"):
+        assert rcp.rcp_kv_attention(q, cache, *args, variant=variant).shape == (0, 4, 64)
+    assert all(same_bits(a, b) for a, b in zip(cache, before))
+    assert rcp.rcp_kv_attention(rand(3, 4, 64), cache, *args).any().item() is False   # rows, all of them of no sequence
