@@ -514,13 +514,14 @@ int rcp_kv_attention_variant(int variant, int polls, const void* q_f16, int64_t 
  *   adapter  int32 [M]; an entry outside 0 .. adapters - 1: none, y is base.
  *   scaling  fp32 [adapters].
  *   base     fp16 [M][N], the projection's output; NULL: zero. May be y (the adapters are added in place).
- *   y        fp16 [M][N]. 1 <= M <= 65535, N >= 1.
+ *   y        fp16 [M][N]. 1 <= M <= 65535, 1 <= N <= RCP_LORA_MAX_N (more: RCP_ERR_LIMIT).
  *   workspace  rcp_lora_workspace_bytes(M, rank) bytes, 16-byte aligned, zero-filled once; every call leaves it ready for
  *            the next. Calls that may overlap on the GPU need one each. One zero-filled buffer, large enough for each, may serve
  *            rcp_lora_add, rcp_kv_attention and the linear calls in turn, in any order, on one stream.
  * Asynchronous on `stream`; allocates nothing.
  */
 #define RCP_LORA_MAX_RANK 128
+#define RCP_LORA_MAX_N (1 << 30)
 size_t rcp_lora_workspace_bytes(int M, int rank);
 int rcp_lora_add(const void* x_f16, int64_t x_stride, const void* a_f16, const void* b_f16, const int32_t* adapter,
                  const float* scaling, const void* base_f16, int M, int N, int K, int rank, int adapters, void* y_f16,

@@ -260,6 +260,7 @@ int rcp_lora_add(const void* x_f16, int64_t x_stride, const void* a_f16, const v
   if (!workspace) return RCP_ERR_WORKSPACE;
   if (M < 1 || M > 65535 || N < 1 || K < 64 || K > 65536 || K % 64 || rank < 8 || rank > RCP_LORA_MAX_RANK || rank % 8 || adapters < 1)
     return RCP_ERR_SHAPE;
+  if (N > RCP_LORA_MAX_N) return RCP_ERR_LIMIT;   // (column indexes go some thousands beyond a row's end)
   if (!stride_ok(x_stride, K, M)) return RCP_ERR_SHAPE;
   if (!aligned16(x_f16) || !aligned16(a_f16) || !aligned16(b_f16) || !aligned16(workspace) || !aligned4(adapter) || !aligned4(scaling) ||
       ((reinterpret_cast<uintptr_t>(base_f16) | reinterpret_cast<uintptr_t>(y_f16)) & 1u))

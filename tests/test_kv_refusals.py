@@ -167,3 +167,10 @@ def test_binding_refuses_an_unknown_attention_kernel(L):
     x = torch.zeros(1, 1, 64, dtype=torch.float16)
     with pytest.raises(KeyError):
         rcp.rcp_kv_attention(x, rcp.make_kv_cache(2, 1, 64, 32, "cpu"), x, x, x, out=x, workspace=x, variant="best")
+
+
+@pytest.mark.parametrize("N", [(1 << 30) + 1, (1 << 31) - 1])
+@pytest.mark.parametrize("M", [2, 65])
+def test_lora_refuses_columns_that_its_indexes_cannot_pass(L, M, N):
+    """The kernels step through a row some thousand columns at a time, so that an index may go that far beyond its end."""
+    assert call(L.rcp_lora_add, LORA, M=M, N=N) == LIMIT
