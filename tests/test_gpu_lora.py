@@ -266,3 +266,43 @@ def test_one_workspace_for_adapters_and_attention(M):
             assert torch.equal(rcp.rcp_lora_add(x, a, b, adapter, scaling, base=base, workspace=ws), want_y)
             assert torch.equal(rcp.rcp_kv_attention(*c, workspace=ws), want)
     assert not ws[:256].any()
+
+
+@pytest.mark.parametrize("M", [40, 97, 200])
+@pytest.mark.parametrize("N", [200, 201])
+@pytest.mark.parametrize("order", ["mixed", "runs"])
+def test_a_bad_number_stays_with_its_token_or_adapter(M, N, order):
+    """Few tokens and tiles of many, rows on 16 bytes and off them: NaN and infinity in a token's activations or an adapter's a or b reach no other request, rows
+    without an adapter keep their base bit for bit, and nothing of an earlier call full of NaN is left in the workspace."""
+    K, R, L = 256, 24, 5
+    x, a, b, _, scaling, base = case(M, N, K, R, L, seed=9)
+    i = torch.arange(M, device=DEV, dtype=torch.int32)
+    adapter = i % (L + 1) - 1 if order == "mixed" else (i * (L + 1) // M).int() - 1
+    ws = rcp.make_lora_workspace(M, R, DEV)
+    nan = torch.full_like(x, math.nan)
+    rcp.rcp_lora_add(nan, a, b, (i % L).int(), scaling, base=base, workspace=ws)
+    bad_tokens = [int(t) for t in torch.nonzero(adapter == 0)[:, 0].tolist()[1:3]]
+    x[bad_tokens[0], 7], x[bad_tokens[1], 9] = math.nan, math.inf
+    a[2, 3, 4], b[3, :, 5] = math.nan, math.nan
+    bad = (adapter == 2) | (adapter == 3)
+    bad[bad_tokens] = True
+    keep = torch.nonzero(~bad)[:, 0]
+    ok = [0, 1, 4]
+    names = torch.full((L + 1,), -1, device=DEV, dtype=torch.int32)
+    names[ok] = torch.arange(3, device=DEV, dtype=torch.int32)
+    for form in ("base", "none", "in place"):
+        y = base.clone() if form == "in place" else None
+        got = rcp.rcp_lora_add(x, a, b, adapter, scaling, base=y if y is not None else base if form == "base" else None, y=y, workspace=ws)
+        want, tol = ref.lora(x[keep], a[ok], b[ok], names[adapter[keep].long()], scaling[ok], None if form == "none" else base[keep])
+        check(got[keep], want, tol)
+        none = adapter < 0
+        assert torch.equal(got[none].view(torch.int16), (torch.zeros_like(base) if form == "none" else base)[none].view(torch.int16))
+
+
+@pytest.mark.parametrize("M,adapters", [(65, 48), (130, 64), (200, 200)])
+def test_many_tokens_with_adapters_of_their_own(M, adapters):
+    """A batch of more tokens than the kernel for few takes, nearly every one with another adapter."""
+    x, a, b, adapter, scaling, base = case(M, 640, 512, 16, adapters, seed=51)
+    if M == adapters:
+        adapter = torch.randperm(M, device=DEV).int()
+    check(rcp.rcp_lora_add(x, a, b, adapter, scaling, base=base), *ref.lora(x, a, b, adapter, scaling, base))
