@@ -81,17 +81,22 @@ int attn_few_rows(int seqs, int kv_heads, int64_t room) {
   return (int)std::max<int64_t>(2 * rcp::kAttnMaxRows, 8000 / segments);
 }
 
-template <int DIM>
-int attn_prompt(const rcp::AttnParams& p, cudaStream_t st) {
+template <int DIM, bool LIMITED>
+int attn_prompt_launch(const rcp::AttnParams& p, cudaStream_t st) {
   using L = rcp::PromptLayout<DIM>;
   static_assert(L::bytes <= 232448, "227 KB of shared memory");
   static std::mutex mu;
   static bool done[kMaxDevices] = {};
-  RCP_CUDA(set_max_smem(rcp::kv_attention_prompt_kernel<DIM>, L::bytes, mu, done));
+  RCP_CUDA(set_max_smem(rcp::kv_attention_prompt_kernel<DIM, LIMITED>, L::bytes, mu, done));
   const int64_t ctas = ((int64_t)p.s.tokens * p.group / rcp::kPromptRows + p.s.seqs) * p.kv_heads;
   if (ctas > INT_MAX) return RCP_ERR_LIMIT;
-  RCP_CUDA(launch_overlapped(rcp::kv_attention_prompt_kernel<DIM>, dim3((unsigned)ctas), dim3(rcp::kPromptThreads), L::bytes, st, p));
+  RCP_CUDA(launch_overlapped(rcp::kv_attention_prompt_kernel<DIM, LIMITED>, dim3((unsigned)ctas), dim3(rcp::kPromptThreads), L::bytes, st, p));
   return RCP_OK;
+}
+
+int attn_prompt(const rcp::AttnParams& p, int dim, bool limited, cudaStream_t st) {
+  if (limited) return dim == 64 ? attn_prompt_launch<64, true>(p, st) : attn_prompt_launch<128, true>(p, st);
+  return dim == 64 ? attn_prompt_launch<64, false>(p, st) : attn_prompt_launch<128, false>(p, st);
 }
 
 // The records of the adapters' tiles stand behind what attention keeps zero in front of its parts (its status and counters; the linear calls' status is the first
@@ -220,7 +225,7 @@ int rcp_kv_attention_variant(int variant, int polls, const void* q_f16, int64_t 
   p.k_scale = k_scale; p.v_scale = v_scale;
   p.out = static_cast<__half*>(out_f16);
   p.status = static_cast<int32_t*>(workspace);
-  p.polls = polls >= 0 ? (uint32_t)polls : rcp::kPromptPolls;
+  p.polls = (uint32_t)polls;
   p.arrived = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(workspace) + rcp::kAttnArrivedAt);
   p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + rcp::kAttnPartsAt);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -228,12 +233,12 @@ int rcp_kv_attention_variant(int variant, int polls, const void* q_f16, int64_t 
   const int64_t room = (int64_t)width * page;
   // (attn_quotient: rows and segments of a sequence below 2^16)
   if (variant == RCP_ATTENTION_SPLIT && (rows > 60000 || (rows + rcp::kAttnMaxRows - 1) / rcp::kAttnMaxRows * kv_heads > 65535)) return RCP_ERR_VARIANT;
-  if (variant == RCP_ATTENTION_PROMPT) return dim == 64 ? attn_prompt<64>(p, st) : attn_prompt<128>(p, st);
+  if (variant == RCP_ATTENTION_PROMPT) return attn_prompt(p, dim, polls >= 0, st);
   if (variant == RCP_ATTENTION_AUTO && rows > attn_few_rows(seqs, kv_heads, room)) {
     // (the prompt kernel runs anyway, and has CTAs free for all that is not as short as single tokens)
     const int few = room <= 1024 ? rcp::kAttnMaxRows : 2 * rcp::kAttnMaxRows;
     p.few = seqs > 1 ? few : 0;
-    const int rc2 = dim == 64 ? attn_prompt<64>(p, st) : attn_prompt<128>(p, st);
+    const int rc2 = attn_prompt(p, dim, polls >= 0, st);
     if (rc2 != RCP_OK || seqs == 1) return rc2;
     rows = few;   // and the sequences with few rows
   }

@@ -44,7 +44,7 @@ struct AttnParams {
   const float *k_scale, *v_scale;
   __half* out;               // [tokens][heads][dim]
   int32_t* status;           // set when a bounded wait gives up
-  uint32_t polls;            // of such a wait
+  uint32_t polls;            // of such a wait, in tests
   int few;                   // sequences with more rows than that are the prompt kernel's, the others the split kernel's (0: one kernel has all)
   int32_t* arrived;          // [2][kAttnMaxCtas], zero between calls: of segments, of groups of CTAs
   float* parts;              // [kAttnMaxCtas][2][rows][dim + 2]

@@ -28,7 +28,7 @@ namespace rcp {
 
 constexpr int kPromptThreads = 512, kPromptRows = 256, kPromptKeys = 64, kPromptStages = 4;
 
-constexpr uint32_t kPromptPolls = 1u << 18;   // p.polls as a rule: a wait of this kernel is a few microseconds
+constexpr uint32_t kPromptPolls = 1u << 18;   // a wait of this kernel is a few microseconds
 
 template <int DIM>
 struct PromptLayout {
@@ -142,7 +142,8 @@ struct PromptBlocks {
   }
 };
 
-template <int DIM>
+// LIMITED: waits of p.polls polls, for tests of giving up (with them for all, 28 bytes of registers are spilled and prompts take 356 us, not 353)
+template <int DIM, bool LIMITED>
 __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(const AttnParams p) {
   using L = PromptLayout<DIM>;
   constexpr int BLOCK_Q = 128 * 128, BLOCK = kPromptKeys * 128;   // bytes of a 64-element block of 128 queries, of a tile's keys
@@ -231,7 +232,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) kv_attention_prompt_kernel(
   blocks.kv = kv; blocks.kv_heads = p.kv_heads; blocks.end = sq.end; blocks.lane = lane;
   constexpr uint32_t kS = 0, kO = 256;   // tensor memory: scores (and weights) of the row tiles, then their sums
   bool ok = true;
-  auto prompt_wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, p.polls); };
+  auto prompt_wait = [&](uint32_t bar, uint32_t parity) { return mbar_wait_warp(bar, parity, LIMITED ? p.polls : kPromptPolls); };
 
   if (warp < 8) {
     // ---------------------------------------------------------------- softmax: a thread a row
