@@ -430,7 +430,8 @@ int rcp_selftest_wait_timeout(void* workspace, int polls, void* stream);
  *                      lengths[b] - 1. A length of zero is allowed, and no new tokens are.
  *   table              int32 [seqs][width]: page of positions i * page .. i * page + page - 1. An entry outside
  *                      0 .. pages - 1 is no page: tokens are not stored there and no keys are found there.
- *   max_new            the most new tokens a sequence has (0: not known). Sets launches up, nothing more; of a sequence that has
+ *   max_new            the most new tokens a sequence has (0: not known). Sets launches up, nothing more (not known, or far too
+ *                      large, a step of single tokens is set up for prompts, which costs time); of a sequence that has
  *                      more, the rest is neither stored nor answered (rows left as they were).
  * starts, lengths and table are read on the device, so a captured call serves every later step whose sizes are the same.
  * A token without a position (lengths[b] below the number of its new tokens) or with one past width * page is not
@@ -477,10 +478,11 @@ int rcp_kv_append(const void* q_f16, int64_t q_stride, const void* k_f16, int64_
  *              for the next. Calls that may overlap on the GPU need one each. Its first word receives a non-zero code if one of
  *              the bounded waits of the kernel for many rows gives up (3: softmax, 4: conversion, 5: issue; 0 otherwise): the
  *              rows that this leaves without a result are NaN then, and so are those of that kernel in later calls until the
- *              buffer is zero-filled again.
+ *              buffer is zero-filled again. The buffer may be rcp_lora_add's too, see there.
  * Nothing behind a sequence's length is read: slots that were never written may hold anything.
- * Scores, maxima and sums in fp32; weights are rounded to fp16 for the product with the values, sums stay in fp32. In the kernel
- * for many rows values go through fp16 relative to the largest scale of their 64 positions: exact within 2^22 of it, nothing
+ * Scores, maxima and sums in fp32; exponentials by the hardware's approximation (2^-22 of a weight); weights are rounded to fp16 for the product with the
+ * values, and their sum is of the rounded ones in the kernel for few rows, of unrounded ones in the kernel for many. In the latter,
+ * values go through fp16 relative to the largest scale of their 64 positions: exact within 2^22 of it, nothing
  * is left at 2^32 (blocks of 64 and 128 tokens have one scale there).
  * Asynchronous on `stream`; allocates nothing.
  */

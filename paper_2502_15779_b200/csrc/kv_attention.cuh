@@ -21,8 +21,8 @@
 //   has of a segment (the keys of one sequence, row tile and key head) in part goes to shared memory; the CTA joins what its
 //   warps have, and of a segment that goes on in other CTAs the last one to arrive joins the parts, in their order (so results repeat).
 //   Measured (us, GB/s of what has to be read and written): 64 sequences of 8000 keys at most, 32 heads on 8 of 128: 120, 5.9 TB/s; one of
-//   130999 keys, 64 on 8: 53, 5.0; 16 x 4000, 32 on 32: 63, 5.3; five tokens each of 16 x 8000: 58, 3.2 (three columns of rows; the chain of
-//   operations of a tile, some 1000 instructions on two warps a scheduler); one of 777 keys, dim 64: 7.2, of 20: 3.6. A tile takes a warp some 1700 clocks
+//   130999 keys, 64 on 8: 54, 5.0; 16 x 4000, 32 on 32: 63, 5.3; five tokens each of 16 x 8000: 58, 3.2 (three columns of rows; the chain of
+//   operations of a tile, 840 instructions where one column takes 500, on two warps a scheduler with 255 registers each); one of 777 keys, dim 64: 7.2, of 20: 3.6. A tile takes a warp some 1700 clocks
 //   however few there are: that is what short sequences wait for. 12 or 16 warps a CTA (fewer registers, parts to memory) were slower everywhere (16 x 4000:
 //   70), and so was nearly everywhere a tile's scores made ahead of the weights of the one in front.
 #pragma once
@@ -58,7 +58,7 @@ constexpr float kAttnSlack = 6.f, kAttnLift = 8.f, kAttnNoMax = -1e30f;
 constexpr size_t kAttnArrivedAt = 256, kAttnPartsAt = kAttnArrivedAt + 2 * kAttnMaxCtas * sizeof(int32_t);
 constexpr size_t kAttnWorkspaceBytes = kAttnPartsAt + (size_t)kAttnMaxCtas * 2 * kAttnMaxRows * (128 + 2) * sizeof(float);
 
-// tiles in the ring: three, or two where the parts of 24 rows leave no room
+// tiles in the ring: what shared memory has room for beside the parts, five of 64 elements, three of 128 with eight rows, two with more
 template <int DIM, int NT>
 struct AttnLayout {
   static constexpr int stages = DIM == 64 ? 5 : NT == 1 ? 3 : 2;

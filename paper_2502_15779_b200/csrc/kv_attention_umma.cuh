@@ -8,7 +8,9 @@
 // swizzle; values keep their order, keys along the rows, and are read as a transposed operand); two that issue, one a row tile, so that neither
 // waits for the other's softmax; eight for the softmax, one thread a row. The next tile's scores are made while the softmax works on these.
 // Softmax as in kv_attention.cuh: a row's reference moves only when a score is more than kAttnSlack above it, the sums in tensor memory
-// are rescaled then. (The sum of the weights is of fp32 ones here: tensor memory has no column left for it.) The scales of the values' blocks
+// are rescaled then. (The sum of the weights is of fp32 ones here, before they are rounded to fp16 for the product: tensor memory has no column left for
+// it, and adding the rounded ones again would be 64 conversions more in a chain that is what bounds the kernel. So their roundings do not cancel: off by
+// 2.5e-4 of the results' norm, 2.2e-4 in the kernel of few rows, 2.1e-4 for the rounding of the result alone.) The scales of the values' blocks
 // are folded into the fp16 values relative to a power of two, the unit of the sums, which stays while the exponents of a tile's one or two blocks are
 // within -15 .. 7 of it (fp16 holds codes of 2^-9 .. 448 exactly there) and otherwise moves to four above the larger one, less where the smaller one
 // would be out of that range; converters and softmax warps follow the same rule on the same scales, so nothing has to be handed over. (Of two blocks
@@ -17,7 +19,8 @@
 // Bound by the softmax warps' chain of a tile: of 2250 clocks factors and masks take 380, the wait for the scores 195, reading them 87, their
 // maximum 470, exponentials, sums and fp16 1090; the tensor pipe is at work 1280 of them (64 keys of both row tiles; the scores' products are
 // bound by shared memory, 48 clocks each instead of 32), the exponentials' unit 1024. 32 heads on 8, prompts of 2000, 1790 and 1190 tokens behind
-// 3000, 2506 and 2154: 340 us, 836 TFLOP/s; 17 % of it is the last wave of CTAs. Steps: tiles of 128 keys with one tile of scores 446 us; with the 128
+// 3000, 2506 and 2154: 336 us, 848 TFLOP/s; 17 % of it is the last wave of CTAs. 64 wide the softmax has as much to do for half the products: 294 us, 483
+// TFLOP/s (12 bytes of registers are spilled there). Steps: tiles of 128 keys with one tile of scores 446 us; with the 128
 // scores of a row in registers at once (spilled) 529; the next scores read between the exponentials 429 (they are waited for a whole chain too
 // early: the place they go to is free only when the weights in it have been multiplied); two threads a row, sixteen softmax warps, 381.
 #pragma once

@@ -421,7 +421,7 @@ __global__ void __launch_bounds__(kLoraThreads, 2) lora_down_kernel(const LoraPa
   }
 }
 
-constexpr int kUpCols = 128;   // columns of a tile (32 a warp); a CTA has p.up_tiles of them, so many that all CTAs run at once
+constexpr int kUpCols = 128;   // columns of a tile (32 a warp); a CTA has p.up_tiles of them: a few short waves of CTAs (lora_many)
 // shared memory of lora_up_kernel: z, two stages of a tile's rows of b, three of what is added to; rows with gaps against bank conflicts
 template <int STEPS>
 struct UpLayout {
