@@ -306,3 +306,36 @@ def test_many_tokens_with_adapters_of_their_own(M, adapters):
     if M == adapters:
         adapter = torch.randperm(M, device=DEV).int()
     check(rcp.rcp_lora_add(x, a, b, adapter, scaling, base=base), *ref.lora(x, a, b, adapter, scaling, base))
+
+
+def test_one_workspace_for_a_layer():
+    """Linear calls, adapters of few and many tokens and attention of both kernels in turn on one zero-filled buffer."""
+    heads, kv_heads, dim, page, K, N, rank = 8, 2, 64, 64, 512, 768, 16
+    codes, lut = synth.make_layer(N, K, K, "uniform", 5, DEV)
+    words = rcp.rcp_pack_weights(codes)
+    cache = rcp.make_kv_cache(20, kv_heads, dim, page, DEV)
+    k = rand(1200, kv_heads, dim, seed=1)
+    table = torch.arange(19, dtype=torch.int32, device=DEV)[None]
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device=DEV)
+    rcp.rcp_kv_append(k, k, cache, i32(0, 1200), i32(1200), table)
+
+    def linear(x, **ws):
+        n = len(x)
+        xq, scale = torch.empty(n, K // 2, dtype=torch.uint8, device=DEV), torch.empty(n, dtype=torch.float16, device=DEV)
+        return rcp.rcp_linear_w2a4(x, K, 1.0, words, lut, xq=xq, scale=scale, **ws)
+
+    def calls(**ws):
+        out = []
+        for M, new in ((1, 1), (16, 300), (70, 40)):
+            x, a, b, adapter, scaling, _ = case(M, N, K, rank, 4, seed=M)
+            base = torch.cat([linear(x[i:i + 16], **ws) for i in range(0, M, 16)])
+            out.append(rcp.rcp_lora_add(x, a, b, adapter, scaling, base=base, **ws))
+            for variant in ("split", "prompt"):
+                out.append(rcp.rcp_kv_attention(rand(new, heads, dim, seed=new), cache, i32(0, new), i32(1200), table, variant=variant, **ws))
+        return out
+
+    one = torch.zeros(8 << 20, dtype=torch.uint8, device=DEV)
+    want = calls()
+    for _ in range(2):
+        assert all(torch.equal(g, w) for g, w in zip(calls(workspace=one), want))
+    assert not one[:256].any()
