@@ -456,7 +456,7 @@ def rcp_kv_attention(q, cache, starts, lengths, block_table, sm_scale=None, max_
 def kv_attention_status(workspace) -> int:
     """0, or the code that rcp_kv_attention left in its workspace when a wait gave up (3, 4 or 5; zero-fill it to go on). Waits for the calls in
     front of it."""
-    return int(workspace[:4].view(torch.int32))
+    return int(workspace.view(torch.uint8).flatten()[:4].view(torch.int32))
 
 
 def rcp_lora_add(x, a, b, adapter, scaling, base=None, y=None, workspace=None):
